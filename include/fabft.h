@@ -64,10 +64,11 @@ enum {
   FABFT_E_HEADDIM = -3,  /* d is not 64, 96, 128 or 256 */
   FABFT_E_ALIGN = -4,    /* q, k, v or o not 16-byte aligned */
   FABFT_E_LAUNCH = -5,   /* the kernel launch failed */
-  FABFT_E_SCALE = -6,    /* scale negative, NaN or infinite */
+  FABFT_E_SCALE = -6,    /* scale (or decay) negative, NaN or infinite */
   FABFT_E_FAULT = -7,    /* fault descriptor out of range */
   FABFT_E_THRESHOLD = -8, /* threshold negative or NaN */
-  FABFT_E_WORKSPACE = -9, /* workspace smaller than fabft_splitkv_workspace_bytes */
+  FABFT_E_WORKSPACE = -9, /* workspace smaller than fabft_splitkv_workspace_bytes,
+                             or fabft_cache_workspace_bytes */
   FABFT_E_MODE = -10      /* a mode argument outside its documented values */
 };
 
@@ -440,6 +441,108 @@ int fabft_attn_fwd_debug(const void* q, const void* k, const void* v,
                          int B, int H, int Lq, int Lk, int d, int causal,
                          float scale, const fabft_fault* faults, int nfaults,
                          const fabft_debug_out* out);
+
+/*
+ * A key/value cache held in 4 bits, the attention over it, and eviction from
+ * it. A value is a number of the grid 0, 0.5, 1, 1.5, 2, 3, 4, 6 (and its
+ * negatives) times a scale:
+ *  - K: 2^e for each 32 channels of a row, e the smallest integer >= -100 with
+ *    max|x| < 7 * 2^e, but at most 125;
+ *  - V: s for each row, the smallest number of six significant bits with
+ *    s >= max|x| / 6 and s >= 2^-100, but at most 21 * 2^121;
+ * x / scale goes to the nearest number of the grid, ties to the even code. All
+ * values are bf16 numbers. K's 32 channels, or V's row, with a NaN or an
+ * infinity among them read as NaN, and the query rows that see such a key are
+ * flagged FABFT_FLAG_NONFINITE.
+ *
+ * With each row of V the cache keeps the sum of its codes, taken when the row
+ * is appended, which is what the checksum's prediction is made of: besides
+ * faults in the attention the row check then finds V codes (and sums) that
+ * changed in memory since the append. K, and the scales, enter the output and
+ * its prediction alike and are not covered.
+ *
+ * The cache is one caller-owned device buffer of fabft_cache_bytes(B, H,
+ * capacity, d) bytes, 16-byte aligned, whose layout is the library's. H counts
+ * key/value heads; capacity, a multiple of 64 (at most 2^30), is the number of
+ * slots (keys) per head. The library keeps no lengths: every call is told them
+ * in device arrays of B ints, so that it can be captured into a graph whose
+ * replays see their current values. A slot that was never written may hold
+ * anything. All four calls are asynchronous on the library stream.
+ */
+long long fabft_cache_bytes(int B, int H, int capacity, int d);
+
+/*
+ * Row i < n of k and v (bf16, [B, H, n, d]) of sequence b goes to slot
+ * start[b] + i. counts (may be NULL: all n): only rows i < counts[b]. A row
+ * whose slot is not in [0, capacity) is dropped; slots that no row goes to
+ * stay as they were. strides: NULL for contiguous k and v, else a HOST array
+ * of the strides, in elements, of k over b, h and i, and of v over b, h and i:
+ * multiples of 8 (FABFT_E_ALIGN); the channels are contiguous.
+ */
+int fabft_cache_append(void* cache, int B, int H, int capacity, int d,
+                       const void* k, const void* v, int n,
+                       const long long* strides, const int* start,
+                       const int* counts);
+
+/*
+ * The values of slots start[b] + i, i < n, into k and v (bf16, [B, H, n, d],
+ * contiguous); zeros for rows i >= counts[b] and for slots not in
+ * [0, capacity).
+ */
+int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
+                     void* k, void* v, int n, const int* start,
+                     const int* counts);
+
+/*
+ * Flash-ABFT attention over the cache: q, o bf16 [B, H * G, Lq, d], query heads
+ * h * G .. h * G + G - 1 over key/value head h; resid, flags [B, H * G, Lq].
+ * Sequence b has the keys of slots [0, lengths[b]) (clamped to [0, capacity])
+ * and the query rows i < counts[b] (clamped to [0, Lq]; NULL: Lq): rows
+ * behind them are padding and get O = 0, resid = 0, flag 0, as do rows that see
+ * no key. causal != 0: the query rows are the last counts[b] keys of the
+ * sequence, row i sees slots <= lengths[b] - counts[b] + i. O, resid, flags, the
+ * threshold and the weighted check as in fabft_attn_fwd; the score check and
+ * the algorithm setting do not apply. Weights (times V's scale) are rounded to
+ * bf16 for the P V product; o and c use the same ones, l the unrounded.
+ *
+ * weight (may be NULL): fp32 [B, H, capacity]; for every slot k < lengths[b]
+ *   weight_k <- decay * weight_k + sum of P_ik over the rows of the G heads
+ * with P_ik the softmax weight of key k in row i. Rows with a flag add nothing.
+ * decay (finite, >= 0; else FABFT_E_SCALE) 0 overwrites. Slots from lengths[b] on
+ * stay as they were. Each slot's sum has one fixed order.
+ *
+ * nsplit: 1..64 ranges of whole 64-key tiles per row, merged by a second
+ * launch; fabft_cache_splits gives the library's choice. A workspace
+ * (16-byte aligned, overwritten) of fabft_cache_workspace_bytes bytes is needed
+ * where that is not 0 (nsplit > 1, or with weight). H * G, B * H * G * Lq and
+ * the grid must fit 31 bits (FABFT_E_SHAPE).
+ */
+int fabft_attn_fwd_cache(const void* q, const void* cache, void* o,
+                         float* resid, uint8_t* flags, int B, int H, int G,
+                         int Lq, int capacity, int d, const int* lengths,
+                         const int* counts, int causal, float scale,
+                         float* weight, float decay, int nsplit,
+                         void* workspace, long long workspace_bytes);
+int fabft_cache_splits(int B, int H, int G, int Lq, int capacity);
+long long fabft_cache_workspace_bytes(int B, int H, int G, int Lq, int d,
+                                      int nsplit, int with_weight);
+
+/*
+ * Eviction: every head of sequence b keeps min(lengths[b], keep) of its slots:
+ * the last min(recent, keep) ones, and of the others those with the largest
+ * weight (equal ones: the lowest slot; a NaN counts as larger than all). They
+ * move, in their order, to the slots from 0 on, with their weights; weights
+ * behind them become 0. into == cache (then into_capacity == capacity and
+ * into_weight == weight) works in place; else into is another cache of the same
+ * B, H and d, which must not overlap it (FABFT_E_SHAPE), and the cache and its
+ * weights stay as they were. index: int [B, H, keep], each place's former slot,
+ * -1 behind the last. new_lengths: int [B]; it may not be lengths. keep:
+ * 1..into_capacity; recent: 0..keep.
+ */
+int fabft_cache_evict(void* cache, int B, int H, int capacity, int d,
+                      float* weight, const int* lengths, int keep, int recent,
+                      void* into, int into_capacity, float* into_weight,
+                      int* index, int* new_lengths);
 
 /* Human-readable text for a status code (static storage). */
 const char* fabft_status_str(int status);

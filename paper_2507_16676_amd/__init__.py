@@ -13,6 +13,13 @@ q: [B, H, Lq, d], k and v: [B, H, Lk, d], torch.bfloat16 on the GPU,
 contiguous; d in {64, 96, 128, 256}. scale defaults to 1/sqrt(d). Every
 caller-supplied tensor (out=, workspaces) is checked for shape, dtype,
 contiguity and device before the library sees its pointer.
+
+A key/value cache held in 4 bits, for decoding over long contexts:
+
+    cache = cache_new(B, H, capacity, d)                    # H key/value heads
+    cache_append(cache, k, v, start)                        # the new tokens' K and V
+    o, resid, flags = attn_fwd_cache(q, cache, lengths, causal=True, weight=w)
+    index, lengths = cache_evict(cache, w, lengths, keep)   # the keys least looked at
 """
 from __future__ import annotations
 
@@ -118,6 +125,22 @@ def _load() -> ctypes.CDLL:
     L.fabft_attn_fwd_splitkv_noalloc.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i,
                                                  _i, _i, _f, _i]
     L.fabft_attn_fwd_splitkv_noalloc.restype = _i
+    _ll = ctypes.c_longlong
+    L.fabft_cache_bytes.argtypes = [_i, _i, _i, _i]
+    L.fabft_cache_bytes.restype = _ll
+    L.fabft_cache_append.argtypes = [_vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp]
+    L.fabft_cache_append.restype = _i
+    L.fabft_cache_read.argtypes = [_vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp]
+    L.fabft_cache_read.restype = _i
+    L.fabft_cache_splits.argtypes = [_i, _i, _i, _i, _i]
+    L.fabft_cache_splits.restype = _i
+    L.fabft_cache_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i, _i]
+    L.fabft_cache_workspace_bytes.restype = _ll
+    L.fabft_attn_fwd_cache.argtypes = [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp,
+                                       _i, _f, _vp, _f, _i, _vp, _ll]
+    L.fabft_attn_fwd_cache.restype = _i
+    L.fabft_cache_evict.argtypes = [_vp, _i, _i, _i, _i, _vp, _vp, _i, _i, _vp, _i, _vp, _vp, _vp]
+    L.fabft_cache_evict.restype = _i
     L.fabft_recompute_flagged.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i,
                                           _f, _vp, _vp, _i, ctypes.POINTER(_i),
                                           ctypes.POINTER(_i)]
@@ -153,6 +176,9 @@ EXPORTS = ("fabft_attn_fwd", "fabft_attn_fwd_nocheck", "fabft_attn_fwd_twopass",
            "fabft_set_weighted_check", "fabft_get_weighted_check",
            "fabft_set_persistent", "fabft_get_persistent",
            "fabft_set_algorithm", "fabft_get_algorithm",
+           "fabft_cache_bytes", "fabft_cache_append", "fabft_cache_read",
+           "fabft_attn_fwd_cache", "fabft_cache_splits", "fabft_cache_workspace_bytes",
+           "fabft_cache_evict",
            "fabft_key_tile", "fabft_query_tile", "fabft_status_str")
 
 
@@ -495,6 +521,227 @@ def global_check(o, resid):
     return gsum, gflags
 
 
+CACHE_TILE = 64
+
+
+@dataclass(frozen=True)
+class Cache:
+    """A key/value cache held in 4 bits (fabft_cache_bytes in include/fabft.h): `data` is the
+    buffer, its layout the library's; `capacity` the slots per head, a multiple of CACHE_TILE.
+    It keeps no lengths: each call is told them. cache_new makes one."""
+    data: "torch.Tensor"   # noqa: F821  uint8 [B, H, capacity / 64, bytes of a tile]
+    B: int
+    H: int
+    capacity: int
+    d: int
+
+
+def cache_new(B: int, H: int, capacity: int, d: int, device="cuda") -> Cache:
+    """An empty cache for B sequences of H key/value heads of d channels, with at least
+    `capacity` slots (rounded up to a multiple of 64) per head."""
+    B, H, d = int(B), int(H), int(d)
+    capacity = -(-int(capacity) // CACHE_TILE) * CACHE_TILE
+    n = int(_load().fabft_cache_bytes(B, H, capacity, d))
+    _check(min(n, 0), "fabft_cache_bytes")
+    tiles = capacity // CACHE_TILE
+    data = _torch.zeros((B, H, tiles, n // (B * H * tiles)), dtype=_torch.uint8, device=device)
+    if not data.is_cuda:
+        raise ValueError("the cache must be on the GPU")
+    return Cache(data, B, H, capacity, d)
+
+
+def _check_cache(c, name: str = "cache"):
+    if _torch is None:
+        _load()
+    if not isinstance(c, Cache):
+        raise TypeError(f"{name} must be a Cache (cache_new), got {type(c).__name__}")
+    t = c.data
+    n = int(_LIB.fabft_cache_bytes(c.B, c.H, c.capacity, c.d))
+    _check(min(n, 0), "fabft_cache_bytes")
+    if not isinstance(t, _torch.Tensor) or t.dtype is not _torch.uint8 or not t.is_cuda or \
+            not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name}.data must be a contiguous uint8 GPU tensor of {n} bytes")
+    return c
+
+
+def _check_ints(t, name: str, B: int, device):
+    return _check_out(t, name, (B,), _torch.int32, device)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(dev, name: str, *args):
+    """An entry point on dev's current stream, with dev current while it runs: a kernel
+    goes to the device that is current, also on the null stream."""
+    f = getattr(_LIB, name)
+    if _torch.cuda.current_device() == dev.index:
+        _stream(dev)
+        rc = f(*args)
+    else:
+        with _torch.cuda.device(dev):
+            _stream(dev)
+            rc = f(*args)
+    _check(rc, name)
+
+
+def _cache_rows(c, t, name: str):
+    """The strides of new rows [B, H, n, d], 0 along a size of 1."""
+    if not isinstance(t, _torch.Tensor) or t.dtype is not _torch.bfloat16:
+        raise TypeError(f"{name} must be a torch.bfloat16 tensor")
+    if t.dim() != 4 or t.shape[0] != c.B or t.shape[1] != c.H or t.shape[3] != c.d:
+        raise ValueError(f"{name} must be [B={c.B}, H={c.H}, n, d={c.d}], got {tuple(t.shape)}")
+    if t.device != c.data.device:
+        raise ValueError(f"{name} must be on {c.data.device}, got {t.device}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}: the channels must be contiguous")
+    return [0 if t.shape[i] == 1 else t.stride(i) for i in range(3)]
+
+
+def cache_append(cache: Cache, k, v, start, counts=None):
+    """Quantise the rows of k and v (bfloat16 [B, H, n, d]; any strides over B, H and n that are
+    multiples of 8 elements) into slots start[b] + i of the cache; with counts, of rows
+    i < counts[b] only. start, counts: int32 [B] on the GPU. Rows whose slot is not in
+    [0, capacity) are dropped."""
+    c = _check_cache(cache)
+    dev = c.data.device
+    strides = _cache_rows(c, k, "k") + _cache_rows(c, v, "v")
+    if k.shape != v.shape:
+        raise ValueError(f"shape mismatch: k {tuple(k.shape)} v {tuple(v.shape)}")
+    _check_ints(start, "start", c.B, dev)
+    if counts is not None:
+        _check_ints(counts, "counts", c.B, dev)
+    if k.shape[2] == 0:
+        return
+    _call(dev, "fabft_cache_append", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, k.data_ptr(),
+          v.data_ptr(), k.shape[2], (ctypes.c_longlong * 6)(*strides), start.data_ptr(),
+          _at(counts))
+
+
+def cache_read(cache: Cache, start, n: int, counts=None, out=None):
+    """The values of slots start[b] .. start[b] + n - 1 as (k, v), bfloat16 [B, H, n, d] (exact:
+    the cache's values are bfloat16 numbers); zeros for rows i >= counts[b] and outside the
+    cache. out: optional preallocated (k, v)."""
+    c = _check_cache(cache)
+    dev, n = c.data.device, int(n)
+    if n < 0:
+        raise ValueError("n must be >= 0")
+    _check_ints(start, "start", c.B, dev)
+    if counts is not None:
+        _check_ints(counts, "counts", c.B, dev)
+    shape = (c.B, c.H, n, c.d)
+    if out is not None:
+        if len(out) != 2:
+            raise ValueError("out must be (k, v)")
+        k = _check_out(out[0], "out[0] (k)", shape, _torch.bfloat16, dev)
+        v = _check_out(out[1], "out[1] (v)", shape, _torch.bfloat16, dev)
+    else:
+        k, v = (_torch.empty(shape, dtype=_torch.bfloat16, device=dev) for _ in range(2))
+    if n:
+        _call(dev, "fabft_cache_read", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, k.data_ptr(),
+              v.data_ptr(), n, start.data_ptr(), _at(counts))
+    return k, v
+
+
+def cache_splits(B: int, H: int, G: int, Lq: int, capacity: int) -> int:
+    """The split count of attn_fwd_cache calls that name none."""
+    r = _load().fabft_cache_splits(int(B), int(H), int(G), int(Lq), int(capacity))
+    _check(min(r, 0), "fabft_cache_splits")
+    return r
+
+
+def cache_workspace_bytes(B: int, H: int, G: int, Lq: int, d: int, nsplit: int,
+                          with_weight: bool = False) -> int:
+    r = int(_load().fabft_cache_workspace_bytes(int(B), int(H), int(G), int(Lq), int(d), int(nsplit),
+                                                int(bool(with_weight))))
+    _check(min(r, 0), "fabft_cache_workspace_bytes")
+    return r
+
+
+def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
+                   scale: float | None = None, weight=None, decay: float = 1.0,
+                   nsplit: int | None = None, workspace=None, out=None):
+    """Flash-ABFT forward over the 4-bit cache. q: bfloat16 [B, H * G, Lq, d], contiguous, G query
+    heads per key/value head. lengths: int32 [B] on the GPU, the keys of each sequence; counts:
+    int32 [B], its query rows (the others are padding: O = 0, no flag). causal: the query rows are
+    the last counts[b] keys. Returns (o, resid, flags) as attn_fwd.
+
+    weight: optional fp32 [B, H, capacity], updated in place: decay * weight + the softmax weights
+    of each key summed over the rows of its group (decay 0 overwrites; rows with a flag add nothing;
+    slots from lengths[b] on stay as they were). nsplit: ranges of the keys, by default
+    cache_splits(...). workspace: optional GPU tensor of cache_workspace_bytes(...) bytes. out:
+    optional preallocated (o, resid, flags)."""
+    c = _check_cache(cache)
+    dev = c.data.device
+    if not isinstance(q, _torch.Tensor) or q.dtype is not _torch.bfloat16:
+        raise TypeError("q must be a torch.bfloat16 tensor")
+    if q.dim() != 4 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [B, H * G, Lq, d] tensor")
+    if q.device != dev:
+        raise ValueError(f"q must be on {dev}, got {q.device}")
+    B, HG, Lq, d = q.shape
+    G = HG // c.H
+    if B != c.B or d != c.d or G < 1 or G * c.H != HG:
+        raise ValueError(f"shape mismatch: q {tuple(q.shape)}, cache B={c.B} H={c.H} d={c.d}")
+    _check_ints(lengths, "lengths", B, dev)
+    if counts is not None:
+        _check_ints(counts, "counts", B, dev)
+    if weight is not None:
+        _check_out(weight, "weight", (B, c.H, c.capacity), _torch.float32, dev)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    nsplit = cache_splits(B, c.H, G, Lq, c.capacity) if nsplit is None else int(nsplit)
+    need = cache_workspace_bytes(B, c.H, G, Lq, d, nsplit, weight is not None)
+    if workspace is not None:
+        _check_workspace(workspace, "workspace", need, dev)
+    elif need:
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
+    if out is not None:
+        if len(out) != 3:
+            raise ValueError("out must be (o, resid, flags)")
+        o = _check_out(out[0], "out[0] (o)", q.shape, _torch.bfloat16, dev)
+        resid = _check_out(out[1], "out[1] (resid)", (B, HG, Lq), _torch.float32, dev)
+        flags = _check_out(out[2], "out[2] (flags)", (B, HG, Lq), _torch.uint8, dev)
+    else:
+        o, resid, flags = _outputs(q, B, HG, Lq)
+    _call(dev, "fabft_attn_fwd_cache", q.data_ptr(), c.data.data_ptr(), o.data_ptr(),
+          resid.data_ptr(), flags.data_ptr(), B, c.H, G, Lq, c.capacity, d, lengths.data_ptr(),
+          _at(counts), int(bool(causal)), scale, _at(weight), float(decay), nsplit, _at(workspace),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
+    return o, resid, flags
+
+
+def cache_evict(cache: Cache, weight, lengths, keep: int, recent: int = 0, into: Cache | None = None,
+                into_weight=None):
+    """Keep min(lengths[b], keep) slots of every head: the last `recent` ones and those of the
+    others with the largest weight (fp32 [B, H, capacity]; equal ones: the lowest slot). They move,
+    in their order, to the first slots of the cache, their weights with them (0 behind them); with
+    into and into_weight, of another cache, and this one stays as it was. Returns (index int32
+    [B, H, keep], each place's former slot, -1 behind the last; new lengths int32 [B])."""
+    c = _check_cache(cache)
+    dev = c.data.device
+    _check_out(weight, "weight", (c.B, c.H, c.capacity), _torch.float32, dev)
+    _check_ints(lengths, "lengths", c.B, dev)
+    if (into is None) != (into_weight is None):
+        raise ValueError("into and into_weight go together")
+    if into is None:
+        into, into_weight = c, weight
+    else:
+        _check_cache(into, "into")
+        if (into.B, into.H, into.d) != (c.B, c.H, c.d) or into.data.device != dev:
+            raise ValueError("into must have the cache's B, H, d and device")
+        _check_out(into_weight, "into_weight", (c.B, c.H, into.capacity), _torch.float32, dev)
+    keep, recent = int(keep), int(recent)
+    if not 1 <= keep <= into.capacity or not 0 <= recent <= keep:
+        raise ValueError(f"keep must be 1..{into.capacity} and recent 0..keep, got {keep}, {recent}")
+    index = _torch.empty((c.B, c.H, keep), dtype=_torch.int32, device=dev)
+    new = _torch.empty((c.B,), dtype=_torch.int32, device=dev)
+    _call(dev, "fabft_cache_evict", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, weight.data_ptr(),
+          lengths.data_ptr(), keep, recent, into.data.data_ptr(), into.capacity,
+          into_weight.data_ptr(), index.data_ptr(), new.data_ptr())
+    return index, new
+
+
 @dataclass
 class Fault:
     """One single-bit fault for attn_fwd_inject (fields as in fabft_fault)."""
@@ -592,6 +839,8 @@ def attn_fwd_inject(q, k, v, causal: bool = False, scale: float | None = None,
 
 __all__ = ["attn_fwd", "attn_fwd_twopass", "attn_fwd_inject", "attn_fwd_debug", "attn_fwd_splitkv", "splitkv_workspace_bytes",
            "splitkv_default_splits",
+           "Cache", "CACHE_TILE", "cache_new", "cache_append", "cache_read", "cache_splits",
+           "cache_workspace_bytes", "attn_fwd_cache", "cache_evict",
            "global_check", "recompute_flagged", "Fault", "FabftError", "set_threshold",
            "set_score_check", "score_check_workspace_bytes", "get_score_threshold",
            "get_threshold", "set_weighted_check", "get_weighted_check", "set_persistent",

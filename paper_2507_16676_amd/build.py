@@ -26,7 +26,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfabft.so")
-SOURCES = [os.path.join(CSRC, "fabft_kernels.hip"), os.path.join(CSRC, "fabft_api.cpp")]
+SOURCES = [os.path.join(CSRC, "fabft_kernels.hip"), os.path.join(CSRC, "fabft_api.cpp"),
+           os.path.join(CSRC, "fabft_cache.hip")]
 ARCH = "gfx950"
 
 
@@ -70,6 +71,7 @@ def build_cmds(out: str, objdir: str, extra=()) -> list[list[str]]:
     k1_obj = os.path.join(objdir, "fabft_kernels_part1.o")
     k2_obj = os.path.join(objdir, "fabft_kernels_part2.o")
     a_obj = os.path.join(objdir, "fabft_api.o")
+    c_obj = os.path.join(objdir, "fabft_cache.o")
     return [
         [hipcc, "-x", "hip", *COMMON, *KERNEL_FLAGS, *inc, *extra, "-c", SOURCES[0], "-o", k_obj],
         [hipcc, "-x", "hip", *COMMON, *KERNEL_FLAGS, *PART1_FLAGS, *inc, *extra, "-c", SOURCES[0],
@@ -77,7 +79,9 @@ def build_cmds(out: str, objdir: str, extra=()) -> list[list[str]]:
         [hipcc, "-x", "hip", *COMMON, *KERNEL_FLAGS, *PART2_FLAGS, *inc, *extra, "-c", SOURCES[0],
          "-o", k2_obj],
         [hipcc, "-x", "hip", *COMMON, *inc, *extra, "-c", SOURCES[1], "-o", a_obj],
-        [hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, k1_obj, k2_obj, a_obj, "-o", out],
+        [hipcc, "-x", "hip", *COMMON, *KERNEL_FLAGS, *inc, *extra, "-c", SOURCES[2], "-o", c_obj],
+        [hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, k1_obj, k2_obj, a_obj, c_obj,
+         "-o", out],
     ]
 
 

@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "../../include/fabft.h"
+#include "fabft_cache.h"
 #include "fabft_kernels.h"
 
 static_assert(FABFT_MAX_FAULTS == fabft::kMaxFaults, "fault list size");
@@ -514,13 +515,191 @@ const char* fabft_status_str(int status) {
     case FABFT_E_HEADDIM: return "unsupported head dimension (d must be 64, 96, 128 or 256)";
     case FABFT_E_ALIGN: return "q, k, v and o must be 16-byte aligned";
     case FABFT_E_LAUNCH: return "kernel launch failed";
-    case FABFT_E_SCALE: return "scale must be finite and >= 0";
+    case FABFT_E_SCALE: return "scale (and decay) must be finite and >= 0";
     case FABFT_E_FAULT: return "fault descriptor out of range";
     case FABFT_E_THRESHOLD: return "threshold must be >= 0";
     case FABFT_E_WORKSPACE: return "workspace too small (see fabft_splitkv_workspace_bytes)";
     case FABFT_E_MODE: return "mode argument out of range";
     default: return "unknown status";
   }
+}
+
+}  // extern "C"
+
+// ---- the 4-bit cache
+
+namespace {
+
+// Sizes that every cache call has: B, H, capacity and d.
+int cache_ok(const void* cache, int B, int H, int capacity, int d) {
+  if (!cache) return FABFT_E_NULL;
+  if (!head_dim_ok(d)) return FABFT_E_HEADDIM;
+  if (B < 1 || H < 1 || capacity < 1 || capacity % fabft::kCacheTile || capacity > (1 << 30))
+    return FABFT_E_SHAPE;
+  if (static_cast<long long>(B) * H > INT_MAX / 64) return FABFT_E_SHAPE;
+  return aligned16(cache) ? FABFT_OK : FABFT_E_ALIGN;
+}
+
+// the cache's size; sizes as accepted by cache_ok fit (2^25 heads of 2^24 tiles of
+// 2^15 bytes could not: refused as FABFT_E_SHAPE)
+long long cache_size(int B, int H, int capacity, int d) {
+  const __int128 n = static_cast<__int128>(B) * H * (capacity / fabft::kCacheTile) *
+                     fabft::CacheTile(d).bytes();
+  return n > LLONG_MAX / 4 ? FABFT_E_SHAPE : static_cast<long long>(n);
+}
+
+bool overlap(const void* a, long long na, const void* b, long long nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
+}
+
+bool splits_ok(int nsplit) { return nsplit >= 1 && nsplit <= kMaxSplits; }
+
+}  // namespace
+
+extern "C" {
+
+long long fabft_cache_bytes(int B, int H, int capacity, int d) {
+  alignas(16) static const char any[16] = {};
+  const int rc = cache_ok(any, B, H, capacity, d);
+  return rc != FABFT_OK ? rc : cache_size(B, H, capacity, d);
+}
+
+int fabft_cache_append(void* cache, int B, int H, int capacity, int d, const void* k,
+                       const void* v, int n, const long long* strides, const int* start,
+                       const int* counts) {
+  if (!k || !v || !start) return FABFT_E_NULL;
+  int rc = cache_ok(cache, B, H, capacity, d);
+  if (rc != FABFT_OK) return rc;
+  if (n < 1 || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
+  if (!aligned16(k) || !aligned16(v)) return FABFT_E_ALIGN;
+  const long long nd = static_cast<long long>(n) * d;
+  const long long dense[6] = {H * nd, nd, d, H * nd, nd, d};
+  const long long* st = strides ? strides : dense;
+  for (int i = 0; i < 6; ++i)
+    if (st[i] % 8) return FABFT_E_ALIGN;
+  fabft::CacheRows p{};
+  p.cache = static_cast<uint8_t*>(cache);
+  p.k = static_cast<uint16_t*>(const_cast<void*>(k));
+  p.v = static_cast<uint16_t*>(const_cast<void*>(v));
+  p.kb = st[0], p.kh = st[1], p.kn = st[2];
+  p.vb = st[3], p.vh = st[4], p.vn = st[5];
+  p.start = start;
+  p.counts = counts;
+  p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile, p.n = n;
+  rc = fabft::launch_cache_append(p, d, g_stream);
+  return rc == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+}
+
+int fabft_cache_read(const void* cache, int B, int H, int capacity, int d, void* k, void* v, int n,
+                     const int* start, const int* counts) {
+  if (!k || !v || !start) return FABFT_E_NULL;
+  int rc = cache_ok(cache, B, H, capacity, d);
+  if (rc != FABFT_OK) return rc;
+  if (n < 1 || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
+  if (!aligned16(k) || !aligned16(v)) return FABFT_E_ALIGN;
+  fabft::CacheRows p{};
+  p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
+  p.k = static_cast<uint16_t*>(k);
+  p.v = static_cast<uint16_t*>(v);
+  p.start = start;
+  p.counts = counts;
+  p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile, p.n = n;
+  rc = fabft::launch_cache_read(p, d, g_stream);
+  return rc == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+}
+
+int fabft_cache_splits(int B, int H, int G, int Lq, int capacity) {
+  if (B < 1 || H < 1 || G < 1 || Lq < 1 || capacity < 1 || capacity > (1 << 30) ||
+      static_cast<long long>(G) * Lq > INT_MAX)
+    return FABFT_E_SHAPE;
+  return fabft::cache_splits(B, H, G * Lq, (capacity + fabft::kCacheTile - 1) / fabft::kCacheTile);
+}
+
+long long fabft_cache_workspace_bytes(int B, int H, int G, int Lq, int d, int nsplit,
+                                      int with_weight) {
+  if (!head_dim_ok(d)) return FABFT_E_HEADDIM;
+  if (B < 1 || H < 1 || G < 1 || Lq < 1 || !splits_ok(nsplit)) return FABFT_E_SHAPE;
+  const __int128 rows = static_cast<__int128>(B) * H * G * Lq;
+  if (rows > INT_MAX) return FABFT_E_SHAPE;
+  const long long n = static_cast<long long>(rows);
+  return 4 * ((with_weight ? 4 * n : 0) +
+              (nsplit > 1 ? n * nsplit * fabft::cache_record_floats(d) : 0));
+}
+
+int fabft_attn_fwd_cache(const void* q, const void* cache, void* o, float* resid, uint8_t* flags,
+                         int B, int H, int G, int Lq, int capacity, int d, const int* lengths,
+                         const int* counts, int causal, float scale, float* weight, float decay,
+                         int nsplit, void* workspace, long long workspace_bytes) {
+  if (!q || !o || !resid || !flags || !lengths) return FABFT_E_NULL;
+  int rc = cache_ok(cache, B, H, capacity, d);
+  if (rc != FABFT_OK) return rc;
+  if (cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
+  const long long need = fabft_cache_workspace_bytes(B, H, G, Lq, d, nsplit, weight != nullptr);
+  if (need < 0) return static_cast<int>(need);
+  if (!std::isfinite(scale) || scale < 0.f) return FABFT_E_SCALE;
+  if (weight && (!std::isfinite(decay) || decay < 0.f)) return FABFT_E_SCALE;
+  if (need > 0 && !workspace) return FABFT_E_NULL;
+  if (!aligned16(q) || !aligned16(o) || (need > 0 && !aligned16(workspace))) return FABFT_E_ALIGN;
+  if (workspace_bytes < need) return FABFT_E_WORKSPACE;
+  fabft::CacheParams p{};
+  p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
+  p.q = static_cast<const uint16_t*>(q);
+  p.o = static_cast<uint16_t*>(o);
+  p.resid = resid;
+  p.flags = flags;
+  p.lengths = lengths;
+  p.counts = counts;
+  p.weight = weight;
+  p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile;
+  p.Lq = Lq, p.R = G * Lq;
+  float* ws = static_cast<float*>(workspace);
+  p.stats = weight ? ws : nullptr;
+  p.ws = nsplit > 1 ? ws + (weight ? 4LL * B * H * p.R : 0) : nullptr;
+  p.causal = causal != 0;
+  p.nsplit = nsplit;
+  p.n_rt = (p.R + fabft::cache_row_tile(p.R) - 1) / fabft::cache_row_tile(p.R);
+  p.wcheck = g_wcheck;
+  p.sl2 = std::max(scale * kLog2e, 0x1p-126f);   // as in the forward
+  p.decay = decay;
+  p.tau_rel = g_tau_rel;
+  p.tau_abs = g_tau_abs;
+  // the grid
+  if (static_cast<long long>(B) * H * p.n_rt * nsplit > INT_MAX) return FABFT_E_SHAPE;
+  return fabft::launch_cache_attn(p, d, g_stream) == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+}
+
+int fabft_cache_evict(void* cache, int B, int H, int capacity, int d, float* weight,
+                      const int* lengths, int keep, int recent, void* into, int into_capacity,
+                      float* into_weight, int* index, int* new_lengths) {
+  if (!weight || !lengths || !into_weight || !index || !new_lengths) return FABFT_E_NULL;
+  int rc = cache_ok(cache, B, H, capacity, d);
+  if (rc != FABFT_OK) return rc;
+  rc = cache_ok(into, B, H, into_capacity, d);
+  if (rc != FABFT_OK) return rc;
+  const long long size = cache_size(B, H, capacity, d), isize = cache_size(B, H, into_capacity, d);
+  if (size < 0 || isize < 0) return FABFT_E_SHAPE;
+  if (keep < 1 || keep > into_capacity || recent < 0 || recent > keep) return FABFT_E_SHAPE;
+  const long long heads = static_cast<long long>(B) * H;
+  if (into == cache) {
+    if (into_capacity != capacity || into_weight != weight) return FABFT_E_SHAPE;
+  } else if (overlap(cache, size, into, isize) ||
+             overlap(weight, 4 * heads * capacity, into_weight, 4 * heads * into_capacity)) {
+    return FABFT_E_SHAPE;
+  }
+  if (overlap(lengths, 4LL * B, new_lengths, 4LL * B)) return FABFT_E_SHAPE;
+  fabft::CacheEvict p{};
+  p.cache = static_cast<uint8_t*>(cache);
+  p.into = static_cast<uint8_t*>(into);
+  p.weight = weight;
+  p.into_weight = into_weight;
+  p.lengths = lengths;
+  p.new_lengths = new_lengths;
+  p.index = index;
+  p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile;
+  p.into_tiles = into_capacity / fabft::kCacheTile;
+  p.keep = keep, p.recent = recent;
+  return fabft::launch_cache_evict(p, d, g_stream) == 0 ? FABFT_OK : FABFT_E_LAUNCH;
 }
 
 }  // extern "C"

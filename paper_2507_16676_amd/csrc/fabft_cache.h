@@ -1,0 +1,106 @@
+// The 4-bit key/value cache: its layout, shared by the host code and the
+// kernels, and the interface between them.
+#ifndef FABFT_CACHE_H
+#define FABFT_CACHE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fabft {
+
+// The cache of one head is a row of tiles of 64 slots (keys). A tile holds, one
+// part after the other:
+//   K codes    64 rows of d/2 bytes; channel 2j in the low half of byte j
+//   K scales   one byte e per slot and block of 32 channels (value 2^(e - 127),
+//              255: the block is NaN), at kscale_at: the lanes that hold the rows
+//              of an MFMA operand find the scales of their four 16-key blocks in
+//              one 32-bit word
+//   V codes    as K's
+//   V scales   64 bf16
+//   V sums     2 x 64 bf16: hi, then lo; hi + lo is the sum of the row's codes
+//              (before the scale), exactly: hi a multiple of 16, lo of 1/2 below 16
+//   V weighted sums  the same of the sum with signs (-1)^j
+// One tile after the other in memory, so that a step of the attention reads
+// one contiguous piece.
+constexpr int kCacheTile = 64;
+
+struct CacheTile {
+  int d;
+  constexpr explicit CacheTile(int d_) : d(d_) {}
+  constexpr int row() const { return d / 2; }
+  constexpr int blocks() const { return d / 32; }
+  constexpr int kscale() const { return kCacheTile * row(); }
+  constexpr int vcode() const { return kscale() + kCacheTile * blocks(); }
+  constexpr int vscale() const { return vcode() + kCacheTile * row(); }
+  constexpr int vsum() const { return vscale() + 2 * kCacheTile; }
+  constexpr int vwsum() const { return vsum() + 4 * kCacheTile; }
+  constexpr int bytes() const { return vwsum() + 4 * kCacheTile; }
+  // MFMA row m of 16-key block kb of a tile is the key 16 (m >> 2) + 4 kb + (m & 3):
+  // then the lane that holds the scores of rows 4g .. 4g + 3 of all four blocks holds
+  // the keys 16g .. 16g + 15, those whose V the transposed read gives it
+  constexpr int kscale_at(int key, int block) const {
+    const int m = ((key >> 4) << 2) | (key & 3), kb = (key >> 2) & 3;
+    return kscale() + (m * blocks() + block) * 4 + kb;
+  }
+};
+
+struct CacheParams {
+  uint8_t* cache;
+  const uint16_t* q;
+  uint16_t* o;
+  float* resid;
+  uint8_t* flags;
+  const int* lengths;   // [B] keys per sequence
+  const int* counts;    // [B] query rows (new tokens) per sequence, or null: all
+  float* weight;        // [B, H, tiles * 64], or null
+  float* stats;         // per query row 4 floats: m (exp2 domain), 1 / l (0: the row
+                        // adds nothing), its last visible key, unused; null without weight
+  float* ws;            // split records: m, l, c, c_w, o[d]
+  int B, H;             // H: key/value heads
+  int tiles;            // capacity in tiles
+  int Lq, R;            // query rows per query head, per key/value head
+  int causal, nsplit, n_rt;
+  int wcheck;
+  float sl2, decay, tau_rel, tau_abs;
+};
+
+struct CacheRows {   // append, read
+  uint8_t* cache;
+  uint16_t* k;
+  uint16_t* v;
+  long long kb, kh, kn, vb, vh, vn;   // strides in elements
+  const int* start;
+  const int* counts;
+  int B, H, tiles, n;
+};
+
+struct CacheEvict {
+  uint8_t* cache;
+  uint8_t* into;        // == cache: in place
+  float* weight;        // [B, H, tiles * 64]
+  float* into_weight;   // [B, H, into_tiles * 64]
+  const int* lengths;
+  int* new_lengths;     // [B]
+  int* index;           // [B, H, keep]
+  int B, H, tiles, into_tiles, keep, recent;
+};
+
+// Query rows that one workgroup of the attention holds per 16-key-row operand.
+inline int cache_row_tile(int R) { return R <= 16 ? 16 : 32; }
+// Splits of the keys: workgroups for the whole chip, of at least 4 tiles each.
+inline int cache_splits(int B, int H, int R, int tiles) {
+  const long long units = (long long)B * H * ((R + cache_row_tile(R) - 1) / cache_row_tile(R));
+  long long ns = (512 + units - 1) / units;
+  if (ns > (tiles + 3) / 4) ns = (tiles + 3) / 4;
+  return ns > 64 ? 64 : (int)ns;
+}
+inline int cache_record_floats(int d) { return d + 4; }
+
+int launch_cache_append(const CacheRows& p, int d, hipStream_t s);
+int launch_cache_read(const CacheRows& p, int d, hipStream_t s);
+int launch_cache_attn(const CacheParams& p, int d, hipStream_t s);
+int launch_cache_evict(const CacheEvict& p, int d, hipStream_t s);
+
+}  // namespace fabft
+
+#endif

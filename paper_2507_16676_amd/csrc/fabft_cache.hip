@@ -1,0 +1,1038 @@
+// The 4-bit key/value cache on gfx950: append, read, attention with the
+// checksum of Algorithm 3, the keys' accumulated softmax weights, eviction.
+//
+// Values are e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and negatives) times a
+// scale: K in blocks of 32 channels with a power of two, which the conversion
+// instruction multiplies in, V with one scale s per row, which multiplies the
+// softmax weight instead: p' = bf16(p s), o = sum p' code, c = sum p' (sum of
+// codes). Both the codes and their sums are exact in bf16, so o and c differ by the
+// rounding of their fp32 sums alone, as in the bf16 forward. The sums are taken
+// when a row is appended: a V code or sum that changes in memory afterwards fails
+// the check of the rows that see it.
+#include "fabft_cache.h"
+
+#include <climits>
+
+namespace fabft {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+constexpr float kInf = __builtin_inff();
+constexpr float kLazy = 8.0f;   // max drift (exp2 domain) before a rescale, as in the forward
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
+  f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+// The eight codes of x as four bf16 pairs (low half: the even code), times the power
+// of two `scale` (infinity: NaN; checked with a probe on gfx950).
+__device__ __forceinline__ u32x4 decode8(uint32_t x, float scale) {
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
+  return r;
+}
+// 2^(e - 127) from byte i of x; 255: infinity
+__device__ __forceinline__ float scale_of_byte(uint32_t x, int i) {
+  return __uint_as_float(((x >> (8 * i)) & 0xffu) << 23);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dppu(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kXor3 = 0x1B, kXor7 = 0x141, kXor15 = 0x140;
+
+// sum / max over the four lanes that differ in bits 4 and 5 (the same column of a
+// 16x16 MFMA result)
+__device__ __forceinline__ float sum_quad(float x) {
+  x += __shfl_xor(x, 16);
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_quad(float x) {
+  x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+// the test on the bits, which relaxed NaN rules cannot fold away
+__device__ __forceinline__ bool nonfinite_bits(float x) {
+  uint32_t b = __float_as_uint(x);
+  asm volatile("" : "+v"(b));
+  return (b & 0x7f800000u) == 0x7f800000u;
+}
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// ---- a row's codes
+
+// sum over aligned groups of N (8, 16 or 32) lanes
+template <int N>
+__device__ __forceinline__ float span_sum(float x) {
+  x += dpp<kXor1>(x);
+  x += dpp<kXor2>(x);
+  x += dpp<kXor7>(x);
+  if constexpr (N >= 16) x += dpp<kXor15>(x);
+  if constexpr (N >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+template <int N>
+__device__ __forceinline__ uint32_t span_max(uint32_t x) {
+  x = max(x, dppu<kXor1>(x));
+  x = max(x, dppu<kXor2>(x));
+  if constexpr (N >= 8) x = max(x, dppu<kXor7>(x));
+  if constexpr (N >= 16) x = max(x, dppu<kXor15>(x));
+  if constexpr (N >= 32) x = max(x, (uint32_t)__shfl_xor((int)x, 16));
+  return x;
+}
+__device__ __forceinline__ uint32_t max_abs8(u32x4 x) {   // of eight bf16, as bits
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m = max(m, x[i] & 0x7fffu);
+    m = max(m, (x[i] >> 16) & 0x7fffu);
+  }
+  return m;
+}
+
+// Lanes of a row of D channels, eight each; 96 channels take 12 of 16 lanes.
+template <int D>
+struct RowLanes {
+  static constexpr int N = D == 96 ? 16 : D / 8;
+  static constexpr int ROWS = 256 / N;   // rows of a workgroup
+};
+
+// ---- append: one row of K and of V per RowLanes<D>::N lanes. Moves 4d bytes in and
+// about d + 14 out per row: bound by memory with many rows, by latency with few.
+template <int D>
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
+  constexpr int N = RowLanes<D>::N;
+  constexpr CacheTile T(D);
+  const int lane = threadIdx.x % N;
+  const long long row = (long long)blockIdx.x * RowLanes<D>::ROWS + threadIdx.x / N;
+  const long long bh = row / p.n;
+  const int i = (int)(row - bh * p.n);
+  if (bh >= (long long)p.B * p.H) return;   // whole groups of N lanes leave together
+  const int b = (int)(bh / p.H), h = (int)(bh - (long long)b * p.H);
+  const long long slot = (long long)p.start[b] + i;
+  if ((p.counts && i >= p.counts[b]) || slot < 0 || slot >= (long long)p.tiles * kCacheTile) return;
+  const bool live = lane < D / 8;
+  u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+  if (live) {
+    k = *reinterpret_cast<const u32x4*>(p.k + b * p.kb + h * p.kh + i * p.kn + 8 * lane);
+    v = *reinterpret_cast<const u32x4*>(p.v + b * p.vb + h * p.vh + i * p.vn + 8 * lane);
+  }
+  uint8_t* tile = p.cache + (bh * p.tiles + slot / kCacheTile) * T.bytes();
+  const int key = (int)(slot % kCacheTile);
+
+  // K: 2^e, the smallest with max < 7 * 2^e: m 2^x with m < 1.75 gives x - 2, else x - 1
+  const uint32_t ka = span_max<4>(max_abs8(k));
+  const bool kbad = ka >= 0x7f80u;
+  // (at most 125: 4 * 2^126 is no number)
+  const int e = kbad ? 255 : clampi((int)(ka >> 7) - 2 + ((ka & 127) >= 96 ? 1 : 0), 27, 252);
+  const float ks = __uint_as_float((uint32_t)(kbad ? 127 : e) << 23);
+  uint32_t kc = 0;
+  {
+    // x / 2^e to the nearest code, ties to the even one. (By value: a bit cast of a vector's
+    // element takes the vector's first one.)
+    const uint32_t k0 = k[0], k1 = k[1], k2 = k[2], k3 = k[3];
+    kc = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(kc, __builtin_bit_cast(bf16x2, k0), ks, 0);
+    kc = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(kc, __builtin_bit_cast(bf16x2, k1), ks, 1);
+    kc = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(kc, __builtin_bit_cast(bf16x2, k2), ks, 2);
+    kc = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(kc, __builtin_bit_cast(bf16x2, k3), ks, 3);
+    if (kbad) kc = 0;
+  }
+
+  // V: s, the smallest number of six significant bits >= max / 6. max has eight bits, so
+  // a quotient that is no such number is 2^-10 or more away from the next one: the
+  // rounding of the division does not change s
+  const uint32_t va = span_max<N>(max_abs8(v));
+  const bool vbad = va >= 0x7f80u;
+  float s = __builtin_fmaxf(__uint_as_float(va << 16) / 6.0f, 0x1p-100f);
+  s = __uint_as_float((__float_as_uint(s) + 0x3ffffu) & ~0x3ffffu);
+  s = __builtin_fminf(s, 0x1.5p+125f);   // (6 s is a bf16 number)
+  if (vbad) s = 1.0f;
+  const float rs = 1.0f / s;
+  uint32_t vc = 0;
+  float sum = 0.f, wsum = 0.f;
+  {
+    // x / s in fp16: x and c s (c a border between codes) have at most 9 bits, so a
+    // quotient is a border itself or at least 2^-9 of it away, and x * (1 / s), off by
+    // 2^-23, rounds to the border or to its right side
+    uint32_t hp[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f16x2 t = {(_Float16)(__uint_as_float(v[j] << 16) * rs),
+                       (_Float16)(__uint_as_float(v[j] & 0xffff0000u) * rs)};
+      hp[j] = __builtin_bit_cast(uint32_t, t);
+    }
+    vc = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(vc, __builtin_bit_cast(f16x2, hp[0]), 1.0f, 0);
+    vc = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(vc, __builtin_bit_cast(f16x2, hp[1]), 1.0f, 1);
+    vc = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(vc, __builtin_bit_cast(f16x2, hp[2]), 1.0f, 2);
+    vc = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(vc, __builtin_bit_cast(f16x2, hp[3]), 1.0f, 3);
+    if (vbad) vc = 0;
+    const u32x4 x = decode8(vc, 1.0f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float even = __uint_as_float(x[j] << 16), odd = __uint_as_float(x[j] & 0xffff0000u);
+      sum += even + odd;
+      wsum += even - odd;
+    }
+    sum = span_sum<N>(sum);     // multiples of 1/2 up to 1536: exact
+    wsum = span_sum<N>(wsum);
+  }
+  if (!live) return;
+  *reinterpret_cast<uint32_t*>(tile + key * T.row() + 4 * lane) = kc;
+  *reinterpret_cast<uint32_t*>(tile + T.vcode() + key * T.row() + 4 * lane) = vc;
+  if ((lane & 3) == 0) tile[T.kscale_at(key, lane / 4)] = (uint8_t)e;
+  // lane 0: the scale, lanes 1 to 4: hi and lo of the sum and of the weighted sum
+  if (lane < 5) {
+    const float x = lane < 3 ? sum : wsum;
+    const float hi = 16.0f * __builtin_floorf(x * 0.0625f);
+    const float y = lane == 0 ? s : (lane & 1) ? hi : x - hi;
+    const uint16_t u = lane == 0 && vbad ? (uint16_t)0x7fc0 : (uint16_t)(__float_as_uint(y) >> 16);
+    *reinterpret_cast<uint16_t*>(tile + T.vscale() + lane * 2 * kCacheTile + 2 * key) = u;
+  }
+}
+
+// ---- read: the values of a row, zeros for rows that are not in the cache
+template <int D>
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheRows p) {
+  constexpr int N = RowLanes<D>::N;
+  constexpr CacheTile T(D);
+  const int lane = threadIdx.x % N;
+  const long long row = (long long)blockIdx.x * RowLanes<D>::ROWS + threadIdx.x / N;
+  const long long bh = row / p.n;
+  const int i = (int)(row - bh * p.n);
+  if (bh >= (long long)p.B * p.H || lane >= D / 8) return;
+  const int b = (int)(bh / p.H);
+  const long long slot = (long long)p.start[b] + i;
+  u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+  if (!(p.counts && i >= p.counts[b]) && slot >= 0 && slot < (long long)p.tiles * kCacheTile) {
+    const uint8_t* tile = p.cache + (bh * p.tiles + slot / kCacheTile) * T.bytes();
+    const int key = (int)(slot % kCacheTile);
+    const uint32_t kc = *reinterpret_cast<const uint32_t*>(tile + key * T.row() + 4 * lane);
+    const uint32_t vc = *reinterpret_cast<const uint32_t*>(tile + T.vcode() + key * T.row() + 4 * lane);
+    const uint32_t e = tile[T.kscale_at(key, lane / 4)];
+    const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + T.vscale() + 2 * key);
+    k = decode8(kc, scale_of_byte(e, 0));
+    const u32x4 x = decode8(vc, 1.0f);
+    const float sf = __uint_as_float(s << 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)   // exact: 6 bits times 2
+      v[j] = pack_bf16x2(__uint_as_float(x[j] << 16) * sf, __uint_as_float(x[j] & 0xffff0000u) * sf);
+  }
+  *reinterpret_cast<u32x4*>(p.k + row * D + 8 * lane) = k;
+  *reinterpret_cast<u32x4*>(p.v + row * D + 8 * lane) = v;
+}
+
+// ---- attention
+
+// What one sequence's query rows see. Row r of a key/value head is row i = r % Lq of one
+// of its query heads; rows i >= cnt are padding and see nothing.
+struct Seen {
+  int len, cnt, off;   // causal: row i sees keys <= off + i
+  __device__ __forceinline__ Seen(const CacheParams& p, int b) {
+    len = clampi(p.lengths[b], 0, p.tiles * kCacheTile);
+    cnt = p.counts ? clampi(p.counts[b], 0, p.Lq) : p.Lq;
+    off = len - cnt;
+  }
+  // the last key that row r sees, -1: none
+  __device__ __forceinline__ int last(const CacheParams& p, int r) const {
+    const int i = r % p.Lq;
+    return r >= p.R || i >= cnt ? -1 : p.causal ? max(-1, off + i) : len - 1;
+  }
+  // number of keys that hold all that rows r0 .. r0 + n - 1 see
+  __device__ __forceinline__ int keys(const CacheParams& p, int r0, int n) const {
+    if (cnt <= 0) return 0;
+    if (!p.causal) return len;
+    const int a = r0 % p.Lq, z = min(p.R - r0, n) - 1 + a;
+    const int i = z < p.Lq ? min(z, cnt - 1) : cnt - 1;
+    return max(0, off + i + 1);
+  }
+};
+// tiles per split of `keys` keys
+__device__ __forceinline__ int split_tiles(int keys, int nsplit) {
+  const int t = (keys + kCacheTile - 1) / kCacheTile;
+  return max(1, (t + nsplit - 1) / nsplit);
+}
+
+// The end of a row, by one wave: O = o / l, pred = c / l, the check against the sum of O
+// (as in the forward: flagged when NOT |r| <= tau_rel * M + tau_abs, M = sum_j |O_j| + |pred|).
+// Lane j holds columns CPL * j .. of o.
+template <int D>
+struct RowEnd {
+  static constexpr int CPL = D == 256 ? 4 : 2;
+  static constexpr int LANES = D / CPL;
+  __device__ static __forceinline__ void run(const CacheParams& p, size_t row, int lane, int last,
+                                             const float (&o)[CPL], float m, float l, float c,
+                                             float cw) {
+    const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;   // (l NaN: NaN)
+    float act = 0.f, absum = 0.f, actw = 0.f, x[CPL];
+#pragma unroll
+    for (int j = 0; j < CPL; ++j) {
+      x[j] = lane < LANES ? o[j] * inv : 0.f;
+      act += x[j];
+      absum += __builtin_fabsf(x[j]);
+      actw += (j & 1) ? -x[j] : x[j];
+    }
+    if (lane < LANES) {
+      uint32_t* to = reinterpret_cast<uint32_t*>(p.o + row * D) + lane * (CPL / 2);
+#pragma unroll
+      for (int j = 0; j < CPL; j += 2) to[j / 2] = pack_bf16x2(x[j], x[j + 1]);
+    }
+    act = wave_sum(act);
+    absum = wave_sum(absum);
+    const float pred = c * inv, r = pred - act;
+    bool bad = nonfinite_bits(r) || nonfinite_bits(absum);
+    uint32_t f = __builtin_fabsf(r) <= p.tau_rel * (absum + __builtin_fabsf(pred)) + p.tau_abs ? 0 : 1;
+    if (p.wcheck) {
+      const float pw = cw * inv, rw = pw - wave_sum(actw);
+      bad = bad || nonfinite_bits(rw);
+      if (!(__builtin_fabsf(rw) <= p.tau_rel * (absum + __builtin_fabsf(pw)) + p.tau_abs)) f |= 4;
+    }
+    if (bad) f |= 3;
+    if (lane == 0) {
+      p.resid[row] = r;
+      p.flags[row] = (uint8_t)f;
+      if (p.stats) {
+        // a row without keys, or with a flag, adds nothing to the weights
+        const bool adds = f == 0 && l > 0.f;
+        f32x4 st = {adds ? m : kInf, adds ? inv : 0.f, __int_as_float(adds ? last : -1), 0.f};
+        *reinterpret_cast<f32x4*>(p.stats + 4 * row) = st;
+      }
+    }
+  }
+};
+
+// One 64-key tile in registers, as it lies in memory.
+template <int D>
+struct TileRegs {
+  static constexpr int KW = D / 32;   // 32-bit words of K per lane and 16-key block
+  static constexpr int VC = D / 32;   // 16-byte chunks of V per lane
+  uint32_t k[4][KW];
+  u32x4 v[VC];
+  uint32_t ks[D == 256 || D == 96 ? 2 : 1];
+  u32x4 vs[2], cs[2];
+};
+
+template <int D>
+struct Lane {   // a lane's offsets in a tile
+  int m, g, koff, ksoff, vsoff, csoff;
+  __device__ __forceinline__ Lane(int lane, bool wcheck) {
+    constexpr CacheTile T(D);
+    m = lane & 15;
+    g = lane >> 4;
+    koff = (16 * (m >> 2) + (m & 3)) * T.row() + g * (D / 8);
+    // first 32-channel block of the lane's D / 4 channels
+    const int blk = D == 64 ? g / 2 : D == 96 ? (3 * g) / 4 : D == 128 ? g : 2 * g;
+    ksoff = T.kscale() + (m * T.blocks() + blk) * 4;
+    vsoff = T.vscale() + 32 * g;
+    // rows 0 and 1 (with the weighted check 2 and 3) of the check's operand; the
+    // other rows hold copies, whose products nothing reads
+    csoff = T.vsum() + (m & (wcheck ? 3 : 1)) * 2 * kCacheTile + 32 * g;
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void load_k(TileRegs<D>& r, const uint8_t* tile, const Lane<D>& ln) {
+  constexpr CacheTile T(D);
+  constexpr int KW = TileRegs<D>::KW;
+#pragma unroll
+  for (int kb = 0; kb < 4; ++kb) {
+    const uint8_t* a = tile + ln.koff + kb * 4 * T.row();
+    if constexpr (KW == 2) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(a);
+      r.k[kb][0] = x[0], r.k[kb][1] = x[1];
+    } else if constexpr (KW == 3) {
+      const uint32_t* x = reinterpret_cast<const uint32_t*>(a);
+      r.k[kb][0] = x[0], r.k[kb][1] = x[1], r.k[kb][2] = x[2];
+    } else {
+#pragma unroll
+      for (int j = 0; j < KW; j += 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a + 4 * j);
+        r.k[kb][j] = x[0], r.k[kb][j + 1] = x[1], r.k[kb][j + 2] = x[2], r.k[kb][j + 3] = x[3];
+      }
+    }
+  }
+  r.ks[0] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff);
+  if constexpr (D == 256) r.ks[1] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff + 4);
+  // at d = 96 the lane's 24 channels lie in at most two blocks, the last of them (3g + 2) / 4
+  if constexpr (D == 96)
+    r.ks[1] = *reinterpret_cast<const uint32_t*>(
+        tile + T.kscale() + (ln.m * T.blocks() + (3 * ln.g + 2) / 4) * 4);
+}
+template <int D>
+__device__ __forceinline__ void load_v(TileRegs<D>& r, const uint8_t* tile, const Lane<D>& ln, int lane) {
+  constexpr CacheTile T(D);
+#pragma unroll
+  for (int j = 0; j < TileRegs<D>::VC; ++j)
+    r.v[j] = *reinterpret_cast<const u32x4*>(tile + T.vcode() + 1024 * j + 16 * lane);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    r.vs[j] = *reinterpret_cast<const u32x4*>(tile + ln.vsoff + 16 * j);
+    r.cs[j] = *reinterpret_cast<const u32x4*>(tile + ln.csoff + 16 * j);
+  }
+}
+// The MFMA operand of channels 8t of the lane in 16-key block kb
+template <int D>
+__device__ __forceinline__ u32x4 k_operand(const TileRegs<D>& r, int kb, int t, int g) {
+  float s;
+  if constexpr (D == 96) {
+    const bool second = t == 2 || (t == 1 && g == 1);   // (3g + t) / 4 is the second block
+    s = scale_of_byte(second ? r.ks[1] : r.ks[0], kb);
+  } else {
+    s = scale_of_byte(r.ks[D == 256 ? t / 4 : 0], kb);
+  }
+  return decode8(r.k[kb][t], s);
+}
+
+// LDS address of 16-byte chunk q of V's codes: 16 bytes of room every 256, so that
+// the 16 rows of a transposed read lie in different banks
+template <int D>
+__device__ __forceinline__ int v_chunk(int q) {
+  return 16 * (D == 96 ? q : q + (q >> 4));
+}
+
+constexpr int kAttnWaves = 4;
+
+// One workgroup: 16 * NT query rows of one key/value head over one split of the keys. Each
+// wave takes whole tiles of 64 keys, every fourth one, straight from memory into registers
+// (K is in the layout of the MFMA operand; V turns through a wave's own piece of LDS
+// with the transposing 4-bit read), and keeps the rows' m, l, c and o; the waves' states
+// meet at the end. S^T = K Q^T and O^T = V^T P^T, as in the forward: a lane holds values
+// of one query row (column n = lane % 16), keys 16g .. 16g + 15 (g = lane / 16).
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_kernel(CacheParams p) {
+  constexpr CacheTile T(D);
+  constexpr int KT = D / 32, CB = D / 16;
+  constexpr int VLDS = D == 96 ? 32 * D : 32 * D + 2 * D;   // bytes of a wave's V (v_chunk)
+  constexpr int RS = D + 4;                                 // floats of a row in the exchange
+  constexpr int XLDS = 16 * RS * 4;
+  __shared__ __align__(16) uint8_t lds[kAttnWaves * (VLDS > XLDS ? VLDS : XLDS)];
+  __shared__ f32x4 st[kAttnWaves][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = blockIdx.x;
+  const int inner = p.n_rt * p.nsplit, heads = p.B * p.H;
+  int bh = id / inner, in = id - bh * inner;
+  if ((heads & 7) == 0) {   // one head's workgroups on one XCD: they share its tiles in the L2
+    const int j = id >> 3;
+    bh = (j / inner) * 8 + (id & 7);
+    in = j % inner;
+  }
+  const int rt = in / p.nsplit, split = in - rt * p.nsplit;
+  const int b = bh / p.H, r0 = rt * 16 * NT;
+  const Seen seen(p, b);
+  const int keys = seen.keys(p, r0, 16 * NT);
+  const int tps = split_tiles(keys, p.nsplit);
+  const int t_end = min((keys + kCacheTile - 1) / kCacheTile, (split + 1) * tps);
+  if (split > 0 && split * tps >= t_end) return;   // no tile: merge does not read this split
+  const Lane<D> ln(lane, p.wcheck != 0);
+  const size_t row0 = (size_t)bh * p.R;
+
+  int last[NT];
+  u32x4 q[NT][KT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = r0 + 16 * n + ln.m;
+    last[n] = seen.last(p, r);
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      q[n][t] = u32x4{0, 0, 0, 0};
+      if (last[n] >= 0)
+        q[n][t] = *reinterpret_cast<const u32x4*>(p.q + (row0 + r) * D + ln.g * (D / 4) + 8 * t);
+    }
+  }
+  // keys that every row sees need no mask; rows that see none do not count
+  int all = INT_MAX;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) all = min(all, last[n] < 0 ? INT_MAX : last[n] + 1);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) all = min(all, __shfl_xor(all, o));
+  all = __builtin_amdgcn_readfirstlane(all);
+
+  float m2[NT], l[NT];
+  f32x4 o[NT][CB], ck[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m2[n] = -kInf;
+    l[n] = 0.f;
+    ck[n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < CB; ++c) o[n][c] = f32x4{0, 0, 0, 0};
+  }
+  const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
+  uint8_t* vl = lds + wave * VLDS;
+
+  auto step = [&](int t, const TileRegs<D>& r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < TileRegs<D>::VC; ++j)
+      *reinterpret_cast<u32x4*>(vl + v_chunk<D>(64 * j + lane)) = r.v[j];
+    f32x4 s[NT][4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const u32x4 a = k_operand<D>(r, kb, kt, ln.g);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][kb] = mfma16(a, q[n][kt], s[n][kb]);
+      }
+    }
+    float sv[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t w = r.vs[j / 8][(j / 2) & 3];
+      sv[j] = __uint_as_float((j & 1) ? w & 0xffff0000u : w << 16);
+    }
+    const bool edge = (t + 1) * kCacheTile > all;
+    u32x4 pp[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int lim = last[n] - t * kCacheTile - 16 * ln.g;   // the row sees keys j <= lim
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          s[n][j / 4][j & 3] = j <= lim ? s[n][j / 4][j & 3] : -kInf;
+      }
+      float mx = s[n][0][0];
+#pragma unroll
+      for (int j = 1; j < 16; ++j) mx = __builtin_fmaxf(mx, s[n][j / 4][j & 3]);
+      if (__any(mx * p.sl2 > m2[n] + kLazy)) {
+        const float mt = max_quad(mx) * p.sl2;
+        const float mn = mt > m2[n] + kLazy ? mt : m2[n];
+        const float alpha = mn == m2[n] ? 1.0f : __builtin_amdgcn_exp2f(m2[n] - mn);
+        l[n] *= alpha;
+        ck[n] *= alpha;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[n][c] *= alpha;
+        m2[n] = mn;
+      }
+      const float nm = m2[n] == -kInf ? 0.f : -m2[n];
+      float pv[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][j / 4][j & 3], p.sl2, nm));
+        l[n] += x;
+        pv[j] = x * sv[j];
+      }
+      if (edge) {   // (the scales of keys that are not seen may be anything)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) pv[j] = j <= lim ? pv[j] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pp[n][j / 4][j & 3] = pack_bf16x2(pv[2 * j], pv[2 * j + 1]);
+    }
+    u32x4 cs[2] = {r.cs[0], r.cs[1]};
+    if ((t + 1) * kCacheTile > seen.len) {
+      // sums of slots that were never written may be anything, NaN among it
+      const int n = seen.len - t * kCacheTile - 16 * ln.g;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        cs[j / 4][j & 3] &= (2 * j < n ? 0xffffu : 0u) | (2 * j + 1 < n ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      ck[n] = mfma16(cs[0], pp[n][0], ck[n]);
+      ck[n] = mfma16(cs[1], pp[n][1], ck[n]);
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      // lane i of a group reads columns 16c .. of key 16g + i and gets column 16c + i
+      // of keys 16g .. 16g + 15
+      const int a = v_chunk<D>((16 * ln.g + ln.m) * (D / 32) + c / 2) + 8 * (c & 1);
+      const i32x2 x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(vl + a));
+      const u32x4 a0 = decode8((uint32_t)x[0], 1.0f), a1 = decode8((uint32_t)x[1], 1.0f);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        o[n][c] = mfma16(a0, pp[n][0], o[n][c]);
+        o[n][c] = mfma16(a1, pp[n][1], o[n][c]);
+      }
+    }
+  };
+
+  int t = split * tps + wave;
+  TileRegs<D> cur, nxt;
+  if (t < t_end) {
+    load_k<D>(cur, base + (size_t)t * T.bytes(), ln);
+    load_v<D>(cur, base + (size_t)t * T.bytes(), ln, lane);
+  }
+  for (; t < t_end; t += kAttnWaves) {
+    if (t + kAttnWaves < t_end) {
+      const uint8_t* tp = base + (size_t)(t + kAttnWaves) * T.bytes();
+      load_k<D>(nxt, tp, ln);
+      load_v<D>(nxt, tp, ln, lane);
+    }
+    step(t, cur);
+    cur = nxt;
+  }
+
+  // the waves' states: m = max_w m_w, x = sum_w x_w 2^(m_w - m), 16 rows at a time
+  float* ex = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    l[n] = sum_quad(l[n]);
+    __syncthreads();   // the LDS is free
+    if (ln.g == 0) {
+      // hi and lo of c, and of c_w
+      st[wave][ln.m] = f32x4{m2[n], l[n], ck[n][0] + ck[n][1], ck[n][2] + ck[n][3]};
+    }
+    if (last[n] >= 0) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+        *reinterpret_cast<f32x4*>(ex + (wave * 16 + ln.m) * RS + 16 * c + 4 * ln.g) = o[n][c];
+    }
+    __syncthreads();
+    constexpr int CPL = RowEnd<D>::CPL;
+    for (int i = wave; i < 16; i += kAttnWaves) {
+      const int r = r0 + 16 * n + i;
+      if (r >= p.R) break;   // wave-uniform, as all below
+      const int lr = seen.last(p, r);
+      float mm = -kInf;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) mm = __builtin_fmaxf(mm, st[w][i][0]);
+      float x[CPL], ls = 0.f, cs = 0.f, cw = 0.f;
+#pragma unroll
+      for (int j = 0; j < CPL; ++j) x[j] = 0.f;
+      if (lr >= 0) {
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) {
+          const f32x4 sw = st[w][i];
+          // a wave without a tile, or whose tiles the row does not see, has l = 0
+          const float f = sw[0] == -kInf ? (nonfinite_bits(sw[1]) ? 1.f : 0.f)
+                                         : __builtin_amdgcn_exp2f(sw[0] - mm);
+          ls = __builtin_fmaf(f, sw[1], ls);
+          cs = __builtin_fmaf(f, sw[2], cs);
+          cw = __builtin_fmaf(f, sw[3], cw);
+          if (lane < RowEnd<D>::LANES) {
+#pragma unroll
+            for (int j = 0; j < CPL; ++j)
+              x[j] = __builtin_fmaf(f, ex[(w * 16 + i) * RS + CPL * lane + j], x[j]);
+          }
+        }
+      }
+      if (p.nsplit == 1) {
+        RowEnd<D>::run(p, row0 + r, lane, lr, x, mm, ls, cs, cw);
+      } else {
+        float* rec = p.ws + ((row0 + r) * p.nsplit + split) * RS;
+        if (lane == 0) *reinterpret_cast<f32x4*>(rec) = f32x4{mm, ls, cs, cw};
+        if (lane < RowEnd<D>::LANES) {
+#pragma unroll
+          for (int j = 0; j < CPL; ++j) rec[4 + CPL * lane + j] = x[j];
+        }
+      }
+    }
+  }
+}
+
+// ---- merge of the splits, one wave per row, as for the bf16 key split
+template <int D>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheParams p, int row_tile) {
+  constexpr int RS = D + 4, CPL = RowEnd<D>::CPL;
+  const int lane = threadIdx.x & 63;
+  const int nrb = (p.R + 3) / 4;
+  const int bh = blockIdx.x / nrb;
+  const int r = (blockIdx.x - bh * nrb) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (r >= p.R) return;
+  const Seen seen(p, bh / p.H);
+  const int keys = seen.keys(p, r / row_tile * row_tile, row_tile);
+  const int tiles = (keys + kCacheTile - 1) / kCacheTile;
+  const int tps = split_tiles(keys, p.nsplit);
+  const int ns = (tiles + tps - 1) / tps;   // the splits that ran
+  const size_t row = (size_t)bh * p.R + r;
+  const float* rec = p.ws + row * p.nsplit * RS;
+  f32x4 hd = {-kInf, 0.f, 0.f, 0.f};
+  if (lane < ns) hd = *reinterpret_cast<const f32x4*>(rec + (size_t)lane * RS);
+  constexpr int U = 8;   // splits whose outputs load together
+  float x[U][CPL], o[CPL];
+#pragma unroll
+  for (int j = 0; j < CPL; ++j) o[j] = 0.f;
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + u < ns && lane < RowEnd<D>::LANES) {
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) x[u][j] = rec[(size_t)(s0 + u) * RS + 4 + CPL * lane + j];
+      }
+  };
+  load(0);
+  const float m = wave_max(hd[0]);
+  const float w = hd[0] == -kInf ? (nonfinite_bits(hd[1]) ? 1.f : 0.f) : __builtin_amdgcn_exp2f(hd[0] - m);
+  const float l = wave_sum(w * hd[1]), c = wave_sum(w * hd[2]), cw = wave_sum(w * hd[3]);
+  for (int s0 = 0; s0 < ns; s0 += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + u < ns) {
+        const float f = __shfl(w, s0 + u);
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) o[j] = __builtin_fmaf(f, x[u][j], o[j]);
+      }
+    if (s0 + U < ns) load(s0 + U);
+  }
+  RowEnd<D>::run(p, row, lane, seen.last(p, r), o, m, l, c, cw);
+}
+
+// ---- the keys' weights: weight_k <- decay * weight_k + sum over the head's rows of
+// 2^(s - m) / l, with the m and l of the finished rows. A second product K Q^T; every key
+// belongs to one wave, so the sums have one order. The scores are those of the
+// attention, bit for bit.
+template <int D>
+__global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int chunks) {
+  constexpr CacheTile T(D);
+  constexpr int KT = D / 32;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.x / chunks, chunk = blockIdx.x - bh * chunks;
+  const Seen seen(p, bh / p.H);
+  const int tiles = (seen.len + kCacheTile - 1) / kCacheTile;
+  const Lane<D> ln(lane, false);
+  const size_t row0 = (size_t)bh * p.R;
+  const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
+  for (int t = chunk * 4 + wave; t < tiles; t += chunks * 4) {
+    TileRegs<D> r;
+    load_k<D>(r, base + (size_t)t * T.bytes(), ln);
+    float* wp = p.weight + ((size_t)bh * p.tiles + t) * kCacheTile + lane;
+    const bool in = t * kCacheTile + lane < seen.len;
+    const float old = in && p.decay != 0.f ? *wp : 0.f;
+    u32x4 a[4][KT];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) a[kb][kt] = k_operand<D>(r, kb, kt, ln.g);
+    float acc[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+    for (int r0 = 0; r0 < p.R; r0 += 16) {
+      const int row = r0 + ln.m;
+      u32x4 q[KT];
+      f32x4 st = {kInf, 0.f, __int_as_float(-1), 0.f};
+      if (row < p.R) st = *reinterpret_cast<const f32x4*>(p.stats + 4 * (row0 + row));
+      const int lim = __float_as_int(st[2]) - t * kCacheTile - 16 * ln.g;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        q[kt] = u32x4{0, 0, 0, 0};
+        if (row < p.R)
+          q[kt] = *reinterpret_cast<const u32x4*>(p.q + (row0 + row) * D + ln.g * (D / 4) + 8 * kt);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) s = mfma16(a[kb][kt], q[kt], s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.sl2, -st[0])) * st[1];
+          acc[4 * kb + i] += 4 * kb + i <= lim ? x : 0.f;
+        }
+      }
+    }
+    // sum over the 16 rows (lanes n) with half the values left after each step: lane n
+    // ends with key 16g + n
+    float y[8], z[4], u[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool hi = ln.m & 8;
+      const float keep = hi ? acc[j + 8] : acc[j], give = hi ? acc[j] : acc[j + 8];
+      y[j] = keep + dpp<kXor15>(give);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool hi = ln.m & 4;
+      const float keep = hi ? y[j + 4] : y[j], give = hi ? y[j] : y[j + 4];
+      z[j] = keep + dpp<kXor7>(give);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const bool hi = ln.m & 2;
+      const float keep = hi ? z[j + 2] : z[j], give = hi ? z[j] : z[j + 2];
+      u[j] = keep + dpp<kXor3>(give);
+    }
+    const bool hi = ln.m & 1;
+    const float keep = hi ? u[1] : u[0], give = hi ? u[0] : u[1];
+    const float sum = keep + dpp<kXor1>(give);
+    if (in) *wp = p.decay != 0.f ? __builtin_fmaf(p.decay, old, sum) : sum;
+  }
+}
+
+template <int D>
+int launch_attn(const CacheParams& p, hipStream_t s) {
+  const int rt = cache_row_tile(p.R);
+  const long long g = (long long)p.B * p.H * p.n_rt * p.nsplit;
+  const long long mg = (long long)p.B * p.H * ((p.R + 3) / 4);
+  if (g > INT_MAX || mg > INT_MAX) return -1;
+  (void)hipGetLastError();
+  if (rt == 16) hipLaunchKernelGGL((cache_attn_kernel<D, 1>), dim3((unsigned)g), dim3(64 * kAttnWaves), 0, s, p);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 2>), dim3((unsigned)g), dim3(64 * kAttnWaves), 0, s, p);
+  if (p.nsplit > 1)
+    hipLaunchKernelGGL((cache_merge_kernel<D>), dim3((unsigned)mg), dim3(256), 0, s, p, rt);
+  if (p.weight) {
+    // about four workgroups per CU, each wave one tile or more
+    const long long heads = (long long)p.B * p.H;
+    const int most = (p.tiles + 3) / 4;
+    long long ch = (1024 + heads - 1) / heads;
+    if (ch > most) ch = most;
+    if (heads * ch > INT_MAX) return -1;
+    hipLaunchKernelGGL((cache_weight_kernel<D>), dim3((unsigned)(heads * ch)), dim3(256), 0, s, p, (int)ch);
+  }
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+// ---- eviction
+
+// Weights in ascending order as unsigned numbers; NaN above all, -0 as 0.
+__device__ __forceinline__ uint32_t order_of(float w) {
+  uint32_t u = __float_as_uint(w);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  if (u == 0x80000000u) u = 0;
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+constexpr int kEvictThreads = 1024;
+
+// One workgroup per head: the slots it keeps, in slot order. The last min(recent, len)
+// slots stay; of the others those with the largest weights, found as a threshold
+// by four passes over 8 bits of the weight each (a histogram of the candidates that
+// share the bits found so far); equal weights at the threshold go by slot.
+__global__ __launch_bounds__(kEvictThreads) void cache_select_kernel(CacheEvict p) {
+  __shared__ int hist[256];
+  __shared__ int wsum[2][kEvictThreads / 64];
+  __shared__ uint32_t sh_prefix;
+  __shared__ int sh_need;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int bh = blockIdx.x, b = bh / p.H;
+  const int len = clampi(p.lengths[b], 0, p.tiles * kCacheTile);
+  const int kept = min(len, p.keep);
+  int* index = p.index + (size_t)bh * p.keep;
+  if (tid == 0 && bh == b * p.H) p.new_lengths[b] = kept;
+  for (int j = kept + tid; j < p.keep; j += kEvictThreads) index[j] = -1;
+  if (len <= p.keep) {
+    for (int j = tid; j < len; j += kEvictThreads) index[j] = j;
+    return;
+  }
+  const float* w = p.weight + (size_t)bh * p.tiles * kCacheTile;
+  const int old = len - min(p.recent, p.keep);   // candidates: slots [0, old)
+  const int want = kept - (len - old);           // of them to keep, < old
+  for (int j = tid; j < len - old; j += kEvictThreads) index[want + j] = old + j;
+  if (want <= 0) return;
+  uint32_t prefix = 0;
+  int need = want;   // how many of the candidates with the prefix to keep
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < old; i += kEvictThreads) {
+      const uint32_t u = order_of(w[i]);
+      if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8)))
+        atomicAdd(&hist[(u >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      // from the top: lane k has bins 255 - 4k .. 252 - 4k
+      int c[4], s = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += c[j] = hist[255 - 4 * lane - j];
+      int before = s;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(before, o);
+        if (lane >= o) before += x;
+      }
+      before -= s;
+      if (before < need && need <= before + s) {   // one lane
+        int j = 0;
+        while (before + c[j] < need) before += c[j++];
+        sh_prefix = prefix | ((uint32_t)(255 - 4 * lane - j) << shift);
+        sh_need = need - before;
+      }
+    }
+    __syncthreads();
+    prefix = sh_prefix;
+    need = sh_need;
+  }
+  // prefix is the threshold: all above it, and the first `need` equal to it
+  int done_gt = 0, done_eq = 0;
+  for (int i0 = 0; i0 < old; i0 += kEvictThreads) {
+    const int i = i0 + tid;
+    const uint32_t u = i < old ? order_of(w[i]) : 0;
+    const bool gt = i < old && u > prefix, eq = i < old && u == prefix;
+    const uint64_t mg = __ballot(gt), me = __ballot(eq);
+    const uint64_t below = (1ull << lane) - 1;
+    __syncthreads();
+    if (lane == 0) {
+      wsum[0][wave] = __popcll(mg);
+      wsum[1][wave] = __popcll(me);
+    }
+    __syncthreads();
+    int ng = done_gt, ne = done_eq, tg = 0, te = 0;
+    for (int k = 0; k < kEvictThreads / 64; ++k) {
+      const int x = wsum[0][k], y = wsum[1][k];
+      if (k < wave) ng += x, ne += y;
+      tg += x, te += y;
+    }
+    ng += __popcll(mg & below);
+    ne += __popcll(me & below);
+    if (gt || (eq && ne < need)) index[ng + min(ne, need)] = i;
+    done_gt += tg;
+    done_eq += te;
+  }
+}
+
+// The kept rows move to their new slots. In place (into == cache) one workgroup per head
+// and half (K, V) takes the rows in order, a batch at a time: a row only moves down, so
+// once a batch is in registers its slots may be written, and no later batch needs them.
+// Into another cache every batch has its own workgroup.
+// Half 0 moves K's codes and scales and the weights, half 1 V's codes, scales and sums.
+template <int D>
+__global__ __launch_bounds__(kEvictThreads) void cache_move_kernel(CacheEvict p, int batches) {
+  constexpr CacheTile T(D);
+  constexpr int CH = D / 32;            // 16-byte chunks of a row's codes
+  constexpr int BATCH = 1024;           // rows
+  constexpr int NC = BATCH * CH / kEvictThreads;
+  const int tid = threadIdx.x;
+  const int part = blockIdx.x & 1;
+  const int chunk = (blockIdx.x >> 1) % batches;
+  const int bh = (blockIdx.x >> 1) / batches;
+  const int len = clampi(p.lengths[bh / p.H], 0, p.tiles * kCacheTile);
+  const int kept = min(len, p.keep);
+  const int* index = p.index + (size_t)bh * p.keep;
+  const uint8_t* src = p.cache + (size_t)bh * p.tiles * T.bytes();
+  uint8_t* dst = p.into + (size_t)bh * p.into_tiles * T.bytes();
+  const float* w = p.weight + (size_t)bh * p.tiles * kCacheTile;
+  float* nw = p.into_weight + (size_t)bh * p.into_tiles * kCacheTile;
+  const int codes = part ? T.vcode() : 0;
+  for (int j0 = chunk * BATCH; j0 < kept; j0 += batches * BATCH) {
+    u32x4 c[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const int e = k * kEvictThreads + tid, j = j0 + e / CH;
+      if (j < kept) {
+        const int i = index[j];
+        c[k] = *reinterpret_cast<const u32x4*>(src + (size_t)(i / kCacheTile) * T.bytes() + codes +
+                                               (i % kCacheTile) * T.row() + 16 * (e % CH));
+      }
+    }
+    // the small parts: one row per thread
+    const int j = j0 + tid;
+    uint8_t ks[T.blocks()];
+    uint16_t vs[5];
+    float wt = 0.f;
+    if (j < kept) {
+      const int i = index[j];
+      const uint8_t* tile = src + (size_t)(i / kCacheTile) * T.bytes();
+      if (part == 0) {
+#pragma unroll
+        for (int k = 0; k < T.blocks(); ++k) ks[k] = tile[T.kscale_at(i % kCacheTile, k)];
+        wt = w[i];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 5; ++k)
+          vs[k] = *reinterpret_cast<const uint16_t*>(tile + T.vscale() + 2 * kCacheTile * k +
+                                                     2 * (i % kCacheTile));
+      }
+    }
+    // every value of the batch has arrived before any slot of it is written
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const int e = k * kEvictThreads + tid, jj = j0 + e / CH;
+      if (jj < kept)
+        *reinterpret_cast<u32x4*>(dst + (size_t)(jj / kCacheTile) * T.bytes() + codes +
+                                  (jj % kCacheTile) * T.row() + 16 * (e % CH)) = c[k];
+    }
+    if (j < kept) {
+      uint8_t* tile = dst + (size_t)(j / kCacheTile) * T.bytes();
+      if (part == 0) {
+#pragma unroll
+        for (int k = 0; k < T.blocks(); ++k) tile[T.kscale_at(j % kCacheTile, k)] = ks[k];
+        nw[j] = wt;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 5; ++k)
+          *reinterpret_cast<uint16_t*>(tile + T.vscale() + 2 * kCacheTile * k +
+                                       2 * (j % kCacheTile)) = vs[k];
+      }
+    }
+  }
+  // the slots behind them have no weight. In place the same workgroup has read all it
+  // needs of them by now
+  if (part == 0)
+    for (int j = kept + chunk * kEvictThreads + tid; j < p.into_tiles * kCacheTile;
+         j += batches * kEvictThreads)
+      nw[j] = 0.f;
+}
+
+template <int D>
+int launch_evict(const CacheEvict& p, hipStream_t s) {
+  const long long heads = (long long)p.B * p.H;
+  const int batches = p.into == p.cache ? 1 : (p.keep + 1023) / 1024;
+  if (heads > INT_MAX || heads * batches * 2 > INT_MAX) return -1;
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)heads), dim3(kEvictThreads), 0, s, p);
+  hipLaunchKernelGGL((cache_move_kernel<D>), dim3((unsigned)(heads * batches * 2)),
+                     dim3(kEvictThreads), 0, s, p, batches);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+template <int D>
+int launch_rows(const CacheRows& p, bool append, hipStream_t s) {
+  const long long rows = (long long)p.B * p.H * p.n;
+  const long long g = (rows + RowLanes<D>::ROWS - 1) / RowLanes<D>::ROWS;
+  if (g > INT_MAX) return -1;
+  (void)hipGetLastError();
+  if (append) hipLaunchKernelGGL((cache_append_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((cache_read_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+}  // namespace
+
+int launch_cache_append(const CacheRows& p, int d, hipStream_t s) {
+  return d == 64 ? launch_rows<64>(p, true, s) : d == 96 ? launch_rows<96>(p, true, s)
+       : d == 128 ? launch_rows<128>(p, true, s) : launch_rows<256>(p, true, s);
+}
+int launch_cache_read(const CacheRows& p, int d, hipStream_t s) {
+  return d == 64 ? launch_rows<64>(p, false, s) : d == 96 ? launch_rows<96>(p, false, s)
+       : d == 128 ? launch_rows<128>(p, false, s) : launch_rows<256>(p, false, s);
+}
+int launch_cache_attn(const CacheParams& p, int d, hipStream_t s) {
+  return d == 64 ? launch_attn<64>(p, s) : d == 96 ? launch_attn<96>(p, s)
+       : d == 128 ? launch_attn<128>(p, s) : launch_attn<256>(p, s);
+}
+int launch_cache_evict(const CacheEvict& p, int d, hipStream_t s) {
+  return d == 64 ? launch_evict<64>(p, s) : d == 96 ? launch_evict<96>(p, s)
+       : d == 128 ? launch_evict<128>(p, s) : launch_evict<256>(p, s);
+}
+
+}  // namespace fabft
