@@ -511,8 +511,8 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * decay (finite, >= 0; else FABFT_E_SCALE) 0 overwrites. Slots from lengths[b] on
  * stay as they were. Each slot's sum has one fixed order.
  *
- * nsplit: 1..64 ranges of whole 64-key tiles per row, merged by a second
- * launch; fabft_cache_splits gives the library's choice. A workspace
+ * nsplit: 1..64 ranges of whole 64-key tiles per row, merged by the last
+ * workgroup of a row to finish; fabft_cache_splits gives the library's choice. A workspace
  * (16-byte aligned, overwritten) of fabft_cache_workspace_bytes bytes is needed
  * where that is not 0 (nsplit > 1, or with weight). H * G, B * H * G * Lq and
  * the grid must fit 31 bits (FABFT_E_SHAPE).

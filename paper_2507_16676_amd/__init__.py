@@ -535,6 +535,14 @@ class Cache:
     capacity: int
     d: int
 
+    def __post_init__(self):
+        n = int(_load().fabft_cache_bytes(self.B, self.H, self.capacity, self.d))
+        _check(min(n, 0), "fabft_cache_bytes")
+        t = self.data
+        if not isinstance(t, _torch.Tensor) or t.dtype is not _torch.uint8 or not t.is_cuda or \
+                not t.is_contiguous() or t.numel() != n:
+            raise ValueError(f"data must be a contiguous uint8 GPU tensor of {n} bytes")
+
 
 def cache_new(B: int, H: int, capacity: int, d: int, device="cuda") -> Cache:
     """An empty cache for B sequences of H key/value heads of d channels, with at least
@@ -545,58 +553,62 @@ def cache_new(B: int, H: int, capacity: int, d: int, device="cuda") -> Cache:
     _check(min(n, 0), "fabft_cache_bytes")
     tiles = capacity // CACHE_TILE
     data = _torch.zeros((B, H, tiles, n // (B * H * tiles)), dtype=_torch.uint8, device=device)
-    if not data.is_cuda:
-        raise ValueError("the cache must be on the GPU")
     return Cache(data, B, H, capacity, d)
 
 
-def _check_cache(c, name: str = "cache"):
-    if _torch is None:
-        _load()
+def _device_of(c, name: str = "cache"):
     if not isinstance(c, Cache):
         raise TypeError(f"{name} must be a Cache (cache_new), got {type(c).__name__}")
-    t = c.data
-    n = int(_LIB.fabft_cache_bytes(c.B, c.H, c.capacity, c.d))
-    _check(min(n, 0), "fabft_cache_bytes")
-    if not isinstance(t, _torch.Tensor) or t.dtype is not _torch.uint8 or not t.is_cuda or \
-            not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{name}.data must be a contiguous uint8 GPU tensor of {n} bytes")
-    return c
+    return c.data.device
 
 
-def _check_ints(t, name: str, B: int, device):
-    return _check_out(t, name, (B,), _torch.int32, device)
+def _at(t, name: str, shape, dtype, device):
+    """The address of a tensor that has to be as _check_out says; None for None."""
+    if t is None:
+        return None
+    if not (isinstance(t, _torch.Tensor) and t.dtype is dtype and t.shape == shape and
+            t.device == device and t.is_contiguous()):
+        _check_out(t, name, shape, dtype, device)
+    return t.data_ptr()
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
+def _needed(t, name: str):
+    if t is None:
+        raise ValueError(f"{name} must be a torch tensor")
+    return t
 
 
-def _call(dev, name: str, *args):
+def _call(dev, name: str, f, *args):
     """An entry point on dev's current stream, with dev current while it runs: a kernel
     goes to the device that is current, also on the null stream."""
-    f = getattr(_LIB, name)
-    if _torch.cuda.current_device() == dev.index:
-        _stream(dev)
+    if _torch._C._cuda_getDevice() == dev.index:
+        _LIB.fabft_set_stream(_raw_stream(dev.index))
         rc = f(*args)
     else:
         with _torch.cuda.device(dev):
-            _stream(dev)
+            _LIB.fabft_set_stream(_raw_stream(dev.index))
             rc = f(*args)
-    _check(rc, name)
+    if rc:
+        _check(rc, name)
 
 
-def _cache_rows(c, t, name: str):
-    """The strides of new rows [B, H, n, d], 0 along a size of 1."""
+@functools.lru_cache(maxsize=64)
+def _strides(*st):
+    return (ctypes.c_longlong * 6)(*st)
+
+
+def _check_rows(c, t, name: str, dev):
+    """New rows [B, H, n, d]. Returns n."""
     if not isinstance(t, _torch.Tensor) or t.dtype is not _torch.bfloat16:
         raise TypeError(f"{name} must be a torch.bfloat16 tensor")
-    if t.dim() != 4 or t.shape[0] != c.B or t.shape[1] != c.H or t.shape[3] != c.d:
-        raise ValueError(f"{name} must be [B={c.B}, H={c.H}, n, d={c.d}], got {tuple(t.shape)}")
-    if t.device != c.data.device:
-        raise ValueError(f"{name} must be on {c.data.device}, got {t.device}")
+    s = t.shape
+    if len(s) != 4 or s[0] != c.B or s[1] != c.H or s[3] != c.d:
+        raise ValueError(f"{name} must be [B={c.B}, H={c.H}, n, d={c.d}], got {tuple(s)}")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}, got {t.device}")
     if t.stride(3) != 1:
         raise ValueError(f"{name}: the channels must be contiguous")
-    return [0 if t.shape[i] == 1 else t.stride(i) for i in range(3)]
+    return s[2]
 
 
 def cache_append(cache: Cache, k, v, start, counts=None):
@@ -604,32 +616,32 @@ def cache_append(cache: Cache, k, v, start, counts=None):
     multiples of 8 elements) into slots start[b] + i of the cache; with counts, of rows
     i < counts[b] only. start, counts: int32 [B] on the GPU. Rows whose slot is not in
     [0, capacity) are dropped."""
-    c = _check_cache(cache)
-    dev = c.data.device
-    strides = _cache_rows(c, k, "k") + _cache_rows(c, v, "v")
-    if k.shape != v.shape:
+    c, dev = cache, _device_of(cache)
+    n, nv = _check_rows(c, k, "k", dev), _check_rows(c, v, "v", dev)
+    if n != nv:
         raise ValueError(f"shape mismatch: k {tuple(k.shape)} v {tuple(v.shape)}")
-    _check_ints(start, "start", c.B, dev)
-    if counts is not None:
-        _check_ints(counts, "counts", c.B, dev)
-    if k.shape[2] == 0:
-        return
-    _call(dev, "fabft_cache_append", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, k.data_ptr(),
-          v.data_ptr(), k.shape[2], (ctypes.c_longlong * 6)(*strides), start.data_ptr(),
-          _at(counts))
+    st = None
+    if not (k.is_contiguous() and v.is_contiguous()):
+        # (0 along a size of 1, whose stride is of no account)
+        st = _strides(*(0 if t.shape[i] == 1 else t.stride(i) for t in (k, v) for i in range(3)))
+    i32, B = _torch.int32, (c.B,)
+    at = _at(_needed(start, "start"), "start", B, i32, dev)
+    cnt = _at(counts, "counts", B, i32, dev)
+    if n:
+        _call(dev, "fabft_cache_append", _LIB.fabft_cache_append, c.data.data_ptr(), c.B, c.H,
+              c.capacity, c.d, k.data_ptr(), v.data_ptr(), n, st, at, cnt)
 
 
 def cache_read(cache: Cache, start, n: int, counts=None, out=None):
     """The values of slots start[b] .. start[b] + n - 1 as (k, v), bfloat16 [B, H, n, d] (exact:
     the cache's values are bfloat16 numbers); zeros for rows i >= counts[b] and outside the
     cache. out: optional preallocated (k, v)."""
-    c = _check_cache(cache)
-    dev, n = c.data.device, int(n)
+    c, dev, n = cache, _device_of(cache), int(n)
     if n < 0:
         raise ValueError("n must be >= 0")
-    _check_ints(start, "start", c.B, dev)
-    if counts is not None:
-        _check_ints(counts, "counts", c.B, dev)
+    i32, B = _torch.int32, (c.B,)
+    at = _at(_needed(start, "start"), "start", B, i32, dev)
+    cnt = _at(counts, "counts", B, i32, dev)
     shape = (c.B, c.H, n, c.d)
     if out is not None:
         if len(out) != 2:
@@ -637,10 +649,11 @@ def cache_read(cache: Cache, start, n: int, counts=None, out=None):
         k = _check_out(out[0], "out[0] (k)", shape, _torch.bfloat16, dev)
         v = _check_out(out[1], "out[1] (v)", shape, _torch.bfloat16, dev)
     else:
-        k, v = (_torch.empty(shape, dtype=_torch.bfloat16, device=dev) for _ in range(2))
+        k = _torch.empty(shape, dtype=_torch.bfloat16, device=dev)
+        v = _torch.empty_like(k)
     if n:
-        _call(dev, "fabft_cache_read", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, k.data_ptr(),
-              v.data_ptr(), n, start.data_ptr(), _at(counts))
+        _call(dev, "fabft_cache_read", _LIB.fabft_cache_read, c.data.data_ptr(), c.B, c.H, c.capacity,
+              c.d, k.data_ptr(), v.data_ptr(), n, at, cnt)
     return k, v
 
 
@@ -659,6 +672,15 @@ def cache_workspace_bytes(B: int, H: int, G: int, Lq: int, d: int, nsplit: int,
     return r
 
 
+@functools.lru_cache(maxsize=256)
+def _cache_plan(B: int, H: int, G: int, Lq: int, capacity: int, d: int, nsplit: int | None,
+                with_weight: bool):
+    """(splits, workspace bytes) of a call, remembered per shape (a pure function)."""
+    if nsplit is None:
+        nsplit = cache_splits(B, H, G, Lq, capacity)
+    return nsplit, cache_workspace_bytes(B, H, G, Lq, d, nsplit, with_weight)
+
+
 def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
                    scale: float | None = None, weight=None, decay: float = 1.0,
                    nsplit: int | None = None, workspace=None, out=None):
@@ -672,8 +694,7 @@ def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
     slots from lengths[b] on stay as they were). nsplit: ranges of the keys, by default
     cache_splits(...). workspace: optional GPU tensor of cache_workspace_bytes(...) bytes. out:
     optional preallocated (o, resid, flags)."""
-    c = _check_cache(cache)
-    dev = c.data.device
+    c, dev = cache, _device_of(cache)
     if not isinstance(q, _torch.Tensor) or q.dtype is not _torch.bfloat16:
         raise TypeError("q must be a torch.bfloat16 tensor")
     if q.dim() != 4 or not q.is_contiguous():
@@ -681,33 +702,35 @@ def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
     if q.device != dev:
         raise ValueError(f"q must be on {dev}, got {q.device}")
     B, HG, Lq, d = q.shape
-    G = HG // c.H
-    if B != c.B or d != c.d or G < 1 or G * c.H != HG:
+    H = c.H
+    G = HG // H
+    if B != c.B or d != c.d or G < 1 or G * H != HG:
         raise ValueError(f"shape mismatch: q {tuple(q.shape)}, cache B={c.B} H={c.H} d={c.d}")
-    _check_ints(lengths, "lengths", B, dev)
-    if counts is not None:
-        _check_ints(counts, "counts", B, dev)
-    if weight is not None:
-        _check_out(weight, "weight", (B, c.H, c.capacity), _torch.float32, dev)
-    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    nsplit = cache_splits(B, c.H, G, Lq, c.capacity) if nsplit is None else int(nsplit)
-    need = cache_workspace_bytes(B, c.H, G, Lq, d, nsplit, weight is not None)
+    i32, f32 = _torch.int32, _torch.float32
+    lens = _at(_needed(lengths, "lengths"), "lengths", (B,), i32, dev)
+    cnt = _at(counts, "counts", (B,), i32, dev)
+    wt = _at(weight, "weight", (B, H, c.capacity), f32, dev)
+    nsplit, need = _cache_plan(B, H, G, Lq, c.capacity, d, None if nsplit is None else int(nsplit),
+                               weight is not None)
+    ws, size = None, 0
     if workspace is not None:
         _check_workspace(workspace, "workspace", need, dev)
+        ws, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     elif need:
         workspace = _torch.empty(need, dtype=_torch.uint8, device=dev)
+        ws, size = workspace.data_ptr(), need
     if out is not None:
         if len(out) != 3:
             raise ValueError("out must be (o, resid, flags)")
         o = _check_out(out[0], "out[0] (o)", q.shape, _torch.bfloat16, dev)
-        resid = _check_out(out[1], "out[1] (resid)", (B, HG, Lq), _torch.float32, dev)
+        resid = _check_out(out[1], "out[1] (resid)", (B, HG, Lq), f32, dev)
         flags = _check_out(out[2], "out[2] (flags)", (B, HG, Lq), _torch.uint8, dev)
     else:
         o, resid, flags = _outputs(q, B, HG, Lq)
-    _call(dev, "fabft_attn_fwd_cache", q.data_ptr(), c.data.data_ptr(), o.data_ptr(),
-          resid.data_ptr(), flags.data_ptr(), B, c.H, G, Lq, c.capacity, d, lengths.data_ptr(),
-          _at(counts), int(bool(causal)), scale, _at(weight), float(decay), nsplit, _at(workspace),
-          0 if workspace is None else workspace.numel() * workspace.element_size())
+    _call(dev, "fabft_attn_fwd_cache", _LIB.fabft_attn_fwd_cache, q.data_ptr(), c.data.data_ptr(),
+          o.data_ptr(), resid.data_ptr(), flags.data_ptr(), B, H, G, Lq, c.capacity, d, lens, cnt,
+          1 if causal else 0, 1.0 / math.sqrt(d) if scale is None else float(scale), wt, float(decay),
+          nsplit, ws, size)
     return o, resid, flags
 
 
@@ -718,27 +741,26 @@ def cache_evict(cache: Cache, weight, lengths, keep: int, recent: int = 0, into:
     in their order, to the first slots of the cache, their weights with them (0 behind them); with
     into and into_weight, of another cache, and this one stays as it was. Returns (index int32
     [B, H, keep], each place's former slot, -1 behind the last; new lengths int32 [B])."""
-    c = _check_cache(cache)
-    dev = c.data.device
-    _check_out(weight, "weight", (c.B, c.H, c.capacity), _torch.float32, dev)
-    _check_ints(lengths, "lengths", c.B, dev)
+    c, dev = cache, _device_of(cache)
+    i32, f32 = _torch.int32, _torch.float32
+    wt = _at(_needed(weight, "weight"), "weight", (c.B, c.H, c.capacity), f32, dev)
+    lens = _at(_needed(lengths, "lengths"), "lengths", (c.B,), i32, dev)
     if (into is None) != (into_weight is None):
         raise ValueError("into and into_weight go together")
     if into is None:
-        into, into_weight = c, weight
+        into, iw = c, wt
     else:
-        _check_cache(into, "into")
-        if (into.B, into.H, into.d) != (c.B, c.H, c.d) or into.data.device != dev:
+        if _device_of(into, "into") != dev or (into.B, into.H, into.d) != (c.B, c.H, c.d):
             raise ValueError("into must have the cache's B, H, d and device")
-        _check_out(into_weight, "into_weight", (c.B, c.H, into.capacity), _torch.float32, dev)
+        iw = _at(into_weight, "into_weight", (c.B, c.H, into.capacity), f32, dev)
     keep, recent = int(keep), int(recent)
     if not 1 <= keep <= into.capacity or not 0 <= recent <= keep:
         raise ValueError(f"keep must be 1..{into.capacity} and recent 0..keep, got {keep}, {recent}")
-    index = _torch.empty((c.B, c.H, keep), dtype=_torch.int32, device=dev)
-    new = _torch.empty((c.B,), dtype=_torch.int32, device=dev)
-    _call(dev, "fabft_cache_evict", c.data.data_ptr(), c.B, c.H, c.capacity, c.d, weight.data_ptr(),
-          lengths.data_ptr(), keep, recent, into.data.data_ptr(), into.capacity,
-          into_weight.data_ptr(), index.data_ptr(), new.data_ptr())
+    index = _torch.empty((c.B, c.H, keep), dtype=i32, device=dev)
+    new = _torch.empty((c.B,), dtype=i32, device=dev)
+    _call(dev, "fabft_cache_evict", _LIB.fabft_cache_evict, c.data.data_ptr(), c.B, c.H, c.capacity,
+          c.d, wt, lens, keep, recent, into.data.data_ptr(), into.capacity, iw, index.data_ptr(),
+          new.data_ptr())
     return index, new
 
 

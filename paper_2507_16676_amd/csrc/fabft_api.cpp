@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -553,6 +555,18 @@ bool overlap(const void* a, long long na, const void* b, long long nb) {
   return x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
 }
 
+// A number other than 0 for a launch, which no other launch of the process has; it starts
+// anywhere, so that what else a workspace may hold hardly equals it.
+unsigned long long next_nonce() {
+  static std::atomic<unsigned long long> n{
+      static_cast<unsigned long long>(
+          std::chrono::steady_clock::now().time_since_epoch().count()) * 0x9e3779b97f4a7c15ull};
+  unsigned long long x;
+  do x = n.fetch_add(1);
+  while (x == 0);
+  return x;
+}
+
 bool splits_ok(int nsplit) { return nsplit >= 1 && nsplit <= kMaxSplits; }
 
 }  // namespace
@@ -623,8 +637,11 @@ long long fabft_cache_workspace_bytes(int B, int H, int G, int Lq, int d, int ns
   const __int128 rows = static_cast<__int128>(B) * H * G * Lq;
   if (rows > INT_MAX) return FABFT_E_SHAPE;
   const long long n = static_cast<long long>(rows);
-  return 4 * ((with_weight ? 4 * n : 0) +
-              (nsplit > 1 ? n * nsplit * fabft::cache_record_floats(d) : 0));
+  // the rows' m and l; records and tickets of the splits
+  const int rt = fabft::cache_row_tile(G * Lq);
+  const long long units = static_cast<long long>(B) * H * ((G * Lq + rt - 1) / rt);
+  return 16 * (with_weight ? n : 0) +
+         (nsplit > 1 ? 4 * n * nsplit * fabft::cache_record_floats(d) + 8 * units * nsplit : 0);
 }
 
 int fabft_attn_fwd_cache(const void* q, const void* cache, void* o, float* resid, uint8_t* flags,
@@ -655,7 +672,13 @@ int fabft_attn_fwd_cache(const void* q, const void* cache, void* o, float* resid
   p.Lq = Lq, p.R = G * Lq;
   float* ws = static_cast<float*>(workspace);
   p.stats = weight ? ws : nullptr;
-  p.ws = nsplit > 1 ? ws + (weight ? 4LL * B * H * p.R : 0) : nullptr;
+  const long long rows = static_cast<long long>(B) * H * p.R;
+  if (nsplit > 1) {
+    p.ws = ws + (weight ? 4 * rows : 0);
+    p.tickets = reinterpret_cast<unsigned long long*>(p.ws + rows * nsplit *
+                                                                 fabft::cache_record_floats(d));
+    p.nonce = next_nonce();
+  }
   p.causal = causal != 0;
   p.nsplit = nsplit;
   p.n_rt = (p.R + fabft::cache_row_tile(p.R) - 1) / fabft::cache_row_tile(p.R);

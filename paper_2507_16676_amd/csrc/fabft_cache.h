@@ -56,6 +56,8 @@ struct CacheParams {
   float* stats;         // per query row 4 floats: m (exp2 domain), 1 / l (0: the row
                         // adds nothing), its last visible key, unused; null without weight
   float* ws;            // split records: m, l, c, c_w, o[d]
+  unsigned long long* tickets;   // per head, row tile and split: the nonce, once it is done
+  unsigned long long nonce;      // of this launch, not 0
   int B, H;             // H: key/value heads
   int tiles;            // capacity in tiles
   int Lq, R;            // query rows per query head, per key/value head
@@ -85,12 +87,16 @@ struct CacheEvict {
   int B, H, tiles, into_tiles, keep, recent;
 };
 
-// Query rows that one workgroup of the attention holds per 16-key-row operand.
-inline int cache_row_tile(int R) { return R <= 16 ? 16 : 32; }
-// Splits of the keys: workgroups for the whole chip, of at least 4 tiles each.
+// Query rows of a workgroup of the attention, for R rows per key/value head.
+inline int cache_row_tile(int R) { return R <= 1 ? 1 : R <= 4 ? 4 : R <= 8 ? 8 : R <= 16 ? 16 : 32; }
+// Splits of the keys of a cache of `tiles` tiles: two workgroups per CU (512) while each has 16
+// tiles or more, four for each of its waves, else one per CU. Measured (us, splits at 512 and
+// at 256 workgroups): 128 heads of 512 tiles 109 113, 64 of 512 30.0 33.4, 128 of 128 30.8
+// 32.0; 32 heads of 65 tiles 13.1 11.8, 64 of 32 13.1 12.7, 8 heads of 512 21.6 18.4.
 inline int cache_splits(int B, int H, int R, int tiles) {
   const long long units = (long long)B * H * ((R + cache_row_tile(R) - 1) / cache_row_tile(R));
   long long ns = (512 + units - 1) / units;
+  if (tiles < 16 * ns) ns = (256 + units - 1) / units;
   if (ns > (tiles + 3) / 4) ns = (tiles + 3) / 4;
   return ns > 64 ? 64 : (int)ns;
 }

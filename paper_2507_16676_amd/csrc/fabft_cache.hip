@@ -63,27 +63,30 @@ __device__ __forceinline__ uint32_t dppu(uint32_t x) {
 }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kXor3 = 0x1B, kXor7 = 0x141, kXor15 = 0x140;
 
-// sum / max over the four lanes that differ in bits 4 and 5 (the same column of a
-// 16x16 MFMA result)
-__device__ __forceinline__ float sum_quad(float x) {
-  x += __shfl_xor(x, 16);
+// over lanes i and i ^ 32
+__device__ __forceinline__ float sum_xor32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float max_quad(float x) {
-  x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+__device__ __forceinline__ float max_xor32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  x += dpp<kXor1>(x);
+  x += dpp<kXor2>(x);
+  x += dpp<kXor7>(x);
+  x += dpp<kXor15>(x);
+  x += __shfl_xor(x, 16);
+  return sum_xor32(x);
 }
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, o));
-  return x;
+  x = __builtin_fmaxf(x, dpp<kXor1>(x));
+  x = __builtin_fmaxf(x, dpp<kXor2>(x));
+  x = __builtin_fmaxf(x, dpp<kXor7>(x));
+  x = __builtin_fmaxf(x, dpp<kXor15>(x));
+  x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+  return max_xor32(x);
 }
 // the test on the bits, which relaxed NaN rules cannot fold away
 __device__ __forceinline__ bool nonfinite_bits(float x) {
@@ -92,6 +95,8 @@ __device__ __forceinline__ bool nonfinite_bits(float x) {
   return (b & 0x7f800000u) == 0x7f800000u;
 }
 
+// by value: a conditional expression of two array elements would keep the array in memory
+__device__ __forceinline__ float pick(bool c, float a, float b) { return c ? a : b; }
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 // ---- a row's codes
@@ -274,18 +279,13 @@ struct Seen {
   }
   // number of keys that hold all that rows r0 .. r0 + n - 1 see
   __device__ __forceinline__ int keys(const CacheParams& p, int r0, int n) const {
-    if (cnt <= 0) return 0;
-    if (!p.causal) return len;
     const int a = r0 % p.Lq, z = min(p.R - r0, n) - 1 + a;
+    if (cnt <= 0 || (z < p.Lq && a >= cnt)) return 0;
+    if (!p.causal) return len;
     const int i = z < p.Lq ? min(z, cnt - 1) : cnt - 1;
     return max(0, off + i + 1);
   }
 };
-// tiles per split of `keys` keys
-__device__ __forceinline__ int split_tiles(int keys, int nsplit) {
-  const int t = (keys + kCacheTile - 1) / kCacheTile;
-  return max(1, (t + nsplit - 1) / nsplit);
-}
 
 // The end of a row, by one wave: O = o / l, pred = c / l, the check against the sum of O
 // (as in the forward: flagged when NOT |r| <= tau_rel * M + tau_abs, M = sum_j |O_j| + |pred|).
@@ -335,20 +335,9 @@ struct RowEnd {
   }
 };
 
-// One 64-key tile in registers, as it lies in memory.
-template <int D>
-struct TileRegs {
-  static constexpr int KW = D / 32;   // 32-bit words of K per lane and 16-key block
-  static constexpr int VC = D / 32;   // 16-byte chunks of V per lane
-  uint32_t k[4][KW];
-  u32x4 v[VC];
-  uint32_t ks[D == 256 || D == 96 ? 2 : 1];
-  u32x4 vs[2], cs[2];
-};
-
 template <int D>
 struct Lane {   // a lane's offsets in a tile
-  int m, g, koff, ksoff, vsoff, csoff;
+  int m, g, koff, ksoff, csoff;
   __device__ __forceinline__ Lane(int lane, bool wcheck) {
     constexpr CacheTile T(D);
     m = lane & 15;
@@ -357,65 +346,107 @@ struct Lane {   // a lane's offsets in a tile
     // first 32-channel block of the lane's D / 4 channels
     const int blk = D == 64 ? g / 2 : D == 96 ? (3 * g) / 4 : D == 128 ? g : 2 * g;
     ksoff = T.kscale() + (m * T.blocks() + blk) * 4;
-    vsoff = T.vscale() + 32 * g;
     // rows 0 and 1 (with the weighted check 2 and 3) of the check's operand; the
     // other rows hold copies, whose products nothing reads
     csoff = T.vsum() + (m & (wcheck ? 3 : 1)) * 2 * kCacheTile + 32 * g;
   }
 };
 
+// K of one 64-key tile in registers, as it lies in memory.
 template <int D>
-__device__ __forceinline__ void load_k(TileRegs<D>& r, const uint8_t* tile, const Lane<D>& ln) {
-  constexpr CacheTile T(D);
-  constexpr int KW = TileRegs<D>::KW;
+struct KRegs {
+  static constexpr int KW = D / 32;   // 32-bit words per lane and 16-key block
+  uint32_t k[4][KW];
+  uint32_t ks[D == 256 || D == 96 ? 2 : 1];
+  __device__ __forceinline__ void load(const uint8_t* tile, const Lane<D>& ln) {
+    constexpr CacheTile T(D);
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb) {
-    const uint8_t* a = tile + ln.koff + kb * 4 * T.row();
-    if constexpr (KW == 2) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(a);
-      r.k[kb][0] = x[0], r.k[kb][1] = x[1];
-    } else if constexpr (KW == 3) {
-      const uint32_t* x = reinterpret_cast<const uint32_t*>(a);
-      r.k[kb][0] = x[0], r.k[kb][1] = x[1], r.k[kb][2] = x[2];
-    } else {
+    for (int kb = 0; kb < 4; ++kb) {
+      const uint8_t* a = tile + ln.koff + kb * 4 * T.row();
+      if constexpr (KW == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(a);
+        k[kb][0] = x[0], k[kb][1] = x[1];
+      } else if constexpr (KW == 3) {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(a);
+        k[kb][0] = x[0], k[kb][1] = x[1], k[kb][2] = x[2];
+      } else {
 #pragma unroll
-      for (int j = 0; j < KW; j += 4) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(a + 4 * j);
-        r.k[kb][j] = x[0], r.k[kb][j + 1] = x[1], r.k[kb][j + 2] = x[2], r.k[kb][j + 3] = x[3];
+        for (int j = 0; j < KW; j += 4) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(a + 4 * j);
+          k[kb][j] = x[0], k[kb][j + 1] = x[1], k[kb][j + 2] = x[2], k[kb][j + 3] = x[3];
+        }
       }
     }
+    ks[0] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff);
+    if constexpr (D == 256) ks[1] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff + 4);
+    // at d = 96 the lane's 24 channels lie in at most two blocks, the last of them (3g + 2) / 4
+    if constexpr (D == 96)
+      ks[1] = *reinterpret_cast<const uint32_t*>(
+          tile + T.kscale() + (ln.m * T.blocks() + (3 * ln.g + 2) / 4) * 4);
   }
-  r.ks[0] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff);
-  if constexpr (D == 256) r.ks[1] = *reinterpret_cast<const uint32_t*>(tile + ln.ksoff + 4);
-  // at d = 96 the lane's 24 channels lie in at most two blocks, the last of them (3g + 2) / 4
-  if constexpr (D == 96)
-    r.ks[1] = *reinterpret_cast<const uint32_t*>(
-        tile + T.kscale() + (ln.m * T.blocks() + (3 * ln.g + 2) / 4) * 4);
-}
-template <int D>
-__device__ __forceinline__ void load_v(TileRegs<D>& r, const uint8_t* tile, const Lane<D>& ln, int lane) {
-  constexpr CacheTile T(D);
+  // the MFMA operand of the lane's channels 8t .. 8t + 7 in 16-key block kb
+  __device__ __forceinline__ u32x4 operand(int kb, int t, int g) const {
+    float s;
+    if constexpr (D == 96) {
+      const bool second = t == 2 || (t == 1 && g == 1);   // (3g + t) / 4 is the second block
+      s = scale_of_byte(second ? ks[1] : ks[0], kb);
+    } else {
+      s = scale_of_byte(ks[D == 256 ? t / 4 : 0], kb);
+    }
+    return decode8(k[kb][t], s);
+  }
+};
+
+// How a workgroup's rows lie on the 16 columns of an MFMA result. RP = 32: two operands of
+// 16 rows; 16: one; fewer: the RP rows repeat over the columns, so that column n has row
+// n % RP, and a lane takes the softmax of VPL = RP of its 16 keys only, the column's share,
+// instead of all for columns that nobody reads; the weights then meet through LDS.
+// (One row, d = 128: 360 -> 225 vector instructions per tile.)
+template <int RP>
+struct Rows {
+  static constexpr int N = RP == 32 ? 2 : 1;          // operands
+  static constexpr int VPL = RP < 16 ? RP : 16;       // keys per lane and tile
+  static constexpr int COLS = RP < 16 ? RP : 16;      // columns with different rows
+};
+
+// V of one tile: the codes as they lie in memory, the scales of the lane's VPL keys, the sums
+// of 16 keys.
+template <int D, int VPL>
+struct VRegs {
+  static constexpr int VC = D / 32;   // 16-byte chunks per lane
+  static constexpr int SW = VPL == 1 ? 1 : VPL / 2;
+  u32x4 v[VC];
+  uint32_t s[SW];
+  u32x4 cs[2];
+  __device__ __forceinline__ void load_codes(const uint8_t* tile, int lane) {
+    constexpr CacheTile T(D);
 #pragma unroll
-  for (int j = 0; j < TileRegs<D>::VC; ++j)
-    r.v[j] = *reinterpret_cast<const u32x4*>(tile + T.vcode() + 1024 * j + 16 * lane);
+    for (int j = 0; j < VC; ++j)
+      v[j] = *reinterpret_cast<const u32x4*>(tile + T.vcode() + 1024 * j + 16 * lane);
+  }
+  // key0: the first of the lane's keys
+  __device__ __forceinline__ void load_scales(const uint8_t* tile, int key0, const Lane<D>& ln) {
+    constexpr CacheTile T(D);
+    const uint8_t* a = tile + T.vscale() + 2 * key0;
+    if constexpr (VPL == 1) {
+      s[0] = *reinterpret_cast<const uint16_t*>(a);
+    } else if constexpr (VPL == 4) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(a);
+      s[0] = x[0], s[1] = x[1];
+    } else {
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    r.vs[j] = *reinterpret_cast<const u32x4*>(tile + ln.vsoff + 16 * j);
-    r.cs[j] = *reinterpret_cast<const u32x4*>(tile + ln.csoff + 16 * j);
+      for (int j = 0; j < SW; j += 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a + 4 * j);
+        s[j] = x[0], s[j + 1] = x[1], s[j + 2] = x[2], s[j + 3] = x[3];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) cs[j] = *reinterpret_cast<const u32x4*>(tile + ln.csoff + 16 * j);
   }
-}
-// The MFMA operand of channels 8t of the lane in 16-key block kb
-template <int D>
-__device__ __forceinline__ u32x4 k_operand(const TileRegs<D>& r, int kb, int t, int g) {
-  float s;
-  if constexpr (D == 96) {
-    const bool second = t == 2 || (t == 1 && g == 1);   // (3g + t) / 4 is the second block
-    s = scale_of_byte(second ? r.ks[1] : r.ks[0], kb);
-  } else {
-    s = scale_of_byte(r.ks[D == 256 ? t / 4 : 0], kb);
+  __device__ __forceinline__ float scale(int j) const {
+    return __uint_as_float((j & 1) ? s[j / 2] & 0xffff0000u : s[j / 2] << 16);
   }
-  return decode8(r.k[kb][t], s);
-}
+};
 
 // LDS address of 16-byte chunk q of V's codes: 16 bytes of room every 256, so that
 // the 16 rows of a transposed read lie in different banks
@@ -424,23 +455,178 @@ __device__ __forceinline__ int v_chunk(int q) {
   return 16 * (D == 96 ? q : q + (q >> 4));
 }
 
+// Of the 16 scores of a lane (keys 16g + j) those of its column's share.
+template <int VPL>
+__device__ __forceinline__ void take_share(const f32x4 (&s)[4], int n, float (&x)[VPL]) {
+  if constexpr (VPL == 16) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = s[j / 4][j & 3];
+  } else {
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = pick(n & 8, s[2 + j / 4][j & 3], s[j / 4][j & 3]);
+    if constexpr (VPL == 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = y[j];
+    } else {
+      float z[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[j] = pick(n & 4, y[j + 4], y[j]);
+      if constexpr (VPL == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = z[j];
+      } else {
+        x[0] = pick(n & 1, pick(n & 2, z[3], z[1]), pick(n & 2, z[2], z[0]));
+      }
+    }
+  }
+}
+
+// sum / max over the lanes that have the same row: columns n, n + COLS, .. of all four groups
+template <int COLS>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int o = COLS; o < 32; o <<= 1) x += __shfl_xor(x, o);
+  return sum_xor32(x);
+}
+template <int COLS>
+__device__ __forceinline__ float row_max(float x) {
+#pragma unroll
+  for (int o = COLS; o < 32; o <<= 1) x = __builtin_fmaxf(x, __shfl_xor(x, o));
+  return max_xor32(x);
+}
+
 constexpr int kAttnWaves = 4;
 
-// One workgroup: 16 * NT query rows of one key/value head over one split of the keys. Each
-// wave takes whole tiles of 64 keys, every fourth one, straight from memory into registers
-// (K is in the layout of the MFMA operand; V turns through a wave's own piece of LDS
-// with the transposing 4-bit read), and keeps the rows' m, l, c and o; the waves' states
-// meet at the end. S^T = K Q^T and O^T = V^T P^T, as in the forward: a lane holds values
-// of one query row (column n = lane % 16), keys 16g .. 16g + 15 (g = lane / 16).
-template <int D, int NT>
-__global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_kernel(CacheParams p) {
+// The splits of a row tile that sees `tiles` tiles: each wave has a tile, and a few tiles stay
+// with one workgroup (a merge costs 2.2 us, a round of tiles 0.9).
+__device__ __forceinline__ int used_splits(int tiles, int nsplit) {
+  return tiles <= 3 * kAttnWaves ? 1 : min(nsplit, (tiles + kAttnWaves - 1) / kAttnWaves);
+}
+
+__device__ __forceinline__ void put(float* a, float x) {
+  __hip_atomic_store(a, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Called by the first wave of each of the n workgroups of a row tile when its records are out;
+// true for one of them, when all are. Each workgroup has a word, which it sets to the
+// launch's nonce (new for every launch that the host makes: nothing has to clear the words
+// before) and then looks at all of them: the last one to set its word sees them all set. Of
+// several that do, the one that takes the nonce out of the first word is meant (all of them
+// merging 16 splits of 32 heads took 10 us longer). It clears the others too, for a captured
+// launch that runs again with its nonce. (A single count of arrivals would have to start at
+// a known value; exchanged into a word with the nonce it takes a round per workgroup: 64
+// splits +70 us.)
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* words, unsigned long long nonce,
+                                               int split, int n, int lane) {
+  if (lane == 0) __hip_atomic_store(words + split, nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // set before any other is read
+  bool set = true;
+  if (lane < n)
+    set = __hip_atomic_load(words + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nonce;
+  if (!__all(set)) return false;
+  int mine = 0;
+  if (lane == 0)
+    mine = __hip_atomic_exchange(words, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nonce;
+  if (!__builtin_amdgcn_readfirstlane(mine)) return false;
+  if (lane < n) __hip_atomic_store(words + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// The splits' records of the workgroup's rows: m = max_s m_s, x = sum_s x_s 2^(m_s - m) for x in
+// {l, o, c, c_w} (c merges like one more column of o, Eq. 10), then the rows' ends. A chain of
+// memory latencies: the heads of all records load together with the first columns (the
+// splits' weights go to st_w), and a thread takes four columns of a row over the splits,
+// eight at a time.
+template <int D>
+__device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& seen, size_t row0, int r0,
+                                             int rows_most, int ns, float* ex, float* st_w) {
+  constexpr int RS = D + 4, C4 = D / 4, CPL = RowEnd<D>::CPL, W = kAttnWaves, K = 16 / W;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int rows = min(rows_most, p.R - r0);
+  for (int b0 = 0; b0 < rows; b0 += 16) {   // 16 rows at a time
+    const int nr = min(16, rows - b0);
+    const float* rec = p.ws + (row0 + r0 + b0) * p.nsplit * RS;
+    f32x4 h[K], x[8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = wave + W * k;
+      h[k] = f32x4{-kInf, 0.f, 0.f, 0.f};
+      if (i < nr && lane < ns)
+        h[k] = *reinterpret_cast<const f32x4*>(rec + ((size_t)i * p.nsplit + lane) * RS);
+    }
+    auto load = [&](int e, int s0) __attribute__((always_inline)) {
+      const int i = e / C4;
+      const float* a = rec + (size_t)i * p.nsplit * RS + 4 + 4 * (e - i * C4);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        x[u] = *reinterpret_cast<const f32x4*>(a + (size_t)min(s0 + u, ns - 1) * RS);
+    };
+    if (tid < nr * C4) load(tid, 0);
+    float m[K], l[K], c[K], cw[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      m[k] = wave_max(h[k][0]);
+      const float w = h[k][0] == -kInf ? (nonfinite_bits(h[k][1]) ? 1.f : 0.f)
+                                       : __builtin_amdgcn_exp2f(h[k][0] - m[k]);
+      l[k] = wave_sum(w * h[k][1]);
+      c[k] = wave_sum(w * h[k][2]);
+      cw[k] = wave_sum(w * h[k][3]);
+      st_w[(wave + W * k) * 64 + lane] = w;
+    }
+    __syncthreads();
+    for (int e = tid; e < nr * C4; e += 64 * W) {
+      const int i = e / C4;
+      f32x4 o = {0, 0, 0, 0};
+      for (int s0 = 0; s0 < ns; s0 += 8) {
+        if (e != tid || s0 > 0) load(e, s0);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if (s0 + u < ns) {
+            const float w = st_w[i * 64 + s0 + u];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(w, x[u][j], o[j]);
+          }
+        }
+      }
+      *reinterpret_cast<f32x4*>(ex + i * RS + 4 * (e - i * C4)) = o;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = wave + W * k;
+      if (i < nr) {
+        float y[CPL];
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) y[j] = lane < RowEnd<D>::LANES ? ex[i * RS + CPL * lane + j] : 0.f;
+        RowEnd<D>::run(p, row0 + r0 + b0 + i, lane, seen.last(p, r0 + b0 + i), y, m[k], l[k], c[k], cw[k]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// One workgroup: up to RP query rows of one key/value head over one split of the keys. Each wave
+// takes whole tiles of 64 keys, straight from memory into registers (K is in the layout
+// of the MFMA operand; V turns through a wave's own piece of LDS with the transposing 4-bit
+// read), and keeps the rows' m, l, c and o; the waves' states meet at the end. S^T = K Q^T and
+// O^T = V^T P^T, as in the forward: a lane holds values of one query row (column
+// n = lane % 16), keys 16g .. 16g + 15 (g = lane / 16). The tiles go round the waves of all
+// splits, so that a wave's first tile depends on nothing that has to be loaded first.
+template <int D, int RP>
+__global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void cache_attn_kernel(CacheParams p) {
   constexpr CacheTile T(D);
-  constexpr int KT = D / 32, CB = D / 16;
+  using R = Rows<RP>;
+  constexpr int KT = D / 32, CB = D / 16, NT = R::N, VPL = R::VPL;
   constexpr int VLDS = D == 96 ? 32 * D : 32 * D + 2 * D;   // bytes of a wave's V (v_chunk)
+  constexpr int PLDS = RP < 16 ? 128 * RP : 0;              // of its weights
   constexpr int RS = D + 4;                                 // floats of a row in the exchange
-  constexpr int XLDS = 16 * RS * 4;
-  __shared__ __align__(16) uint8_t lds[kAttnWaves * (VLDS > XLDS ? VLDS : XLDS)];
+  constexpr int XLDS = R::COLS * RS * 4;
+  __shared__ __align__(16) uint8_t lds[kAttnWaves * (VLDS + PLDS > XLDS ? VLDS + PLDS : XLDS)];
   __shared__ f32x4 st[kAttnWaves][16];
+  __shared__ float st_w[16 * 64];
+  __shared__ int last_one;
+  static_assert(sizeof(lds) >= 16 * RS * 4 || R::COLS < 16, "merge_splits");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int id = blockIdx.x;
@@ -452,34 +638,46 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
     in = j % inner;
   }
   const int rt = in / p.nsplit, split = in - rt * p.nsplit;
-  const int b = bh / p.H, r0 = rt * 16 * NT;
-  const Seen seen(p, b);
-  const int keys = seen.keys(p, r0, 16 * NT);
-  const int tps = split_tiles(keys, p.nsplit);
-  const int t_end = min((keys + kCacheTile - 1) / kCacheTile, (split + 1) * tps);
-  if (split > 0 && split * tps >= t_end) return;   // no tile: merge does not read this split
+  const int b = bh / p.H, r0 = rt * RP;
   const Lane<D> ln(lane, p.wcheck != 0);
+  const int key0 = 16 * ln.g + (RP < 16 ? ln.m / RP * VPL : 0);   // the first of the lane's keys
   const size_t row0 = (size_t)bh * p.R;
+  const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
 
-  int last[NT];
+  // the first tile loads before the lengths are known (every slot of the cache is memory)
+  int t = split * kAttnWaves + wave;
+  KRegs<D> kr;
+  VRegs<D, VPL> vr;
+  if (t < p.tiles) {
+    const uint8_t* tp = base + (size_t)t * T.bytes();
+    kr.load(tp, ln);
+    vr.load_codes(tp, lane);
+    vr.load_scales(tp, key0, ln);
+  }
   u32x4 q[NT][KT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = r0 + 16 * n + ln.m;
-    last[n] = seen.last(p, r);
+    // (columns without a row take another one's, and padding rows whatever they hold:
+    // a column's results depend on its own q alone)
+    const int r = min(r0 + 16 * n + ln.m % R::COLS, p.R - 1);
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      q[n][t] = u32x4{0, 0, 0, 0};
-      if (last[n] >= 0)
-        q[n][t] = *reinterpret_cast<const u32x4*>(p.q + (row0 + r) * D + ln.g * (D / 4) + 8 * t);
-    }
+    for (int kt = 0; kt < KT; ++kt)
+      q[n][kt] = *reinterpret_cast<const u32x4*>(p.q + (row0 + r) * D + ln.g * (D / 4) + 8 * kt);
   }
-  // keys that every row sees need no mask; rows that see none do not count
-  int all = INT_MAX;
+  const Seen seen(p, b);
+  const int keys = seen.keys(p, r0, RP);
+  const int tiles = (keys + kCacheTile - 1) / kCacheTile;
+  const int ns = used_splits(tiles, p.nsplit);
+  if (split >= ns) return;
+  int last[NT];
+  int all = INT_MAX;   // keys below it need no mask: every row that sees any sees them
 #pragma unroll
-  for (int n = 0; n < NT; ++n) all = min(all, last[n] < 0 ? INT_MAX : last[n] + 1);
+  for (int n = 0; n < NT; ++n) {
+    last[n] = seen.last(p, r0 + 16 * n + ln.m % R::COLS);
+    all = min(all, last[n] < 0 ? INT_MAX : last[n] + 1);
+  }
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) all = min(all, __shfl_xor(all, o));
+  for (int o = 1; o < R::COLS; o <<= 1) all = min(all, __shfl_xor(all, o));
   all = __builtin_amdgcn_readfirstlane(all);
 
   float m2[NT], l[NT];
@@ -492,46 +690,49 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[n][c] = f32x4{0, 0, 0, 0};
   }
-  const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
-  uint8_t* vl = lds + wave * VLDS;
+  uint8_t* vl = lds + wave * (VLDS + PLDS);
+  uint8_t* pl = vl + VLDS;
 
-  auto step = [&](int t, const TileRegs<D>& r) __attribute__((always_inline)) {
+  // each part of the next tile loads into the registers of this one as soon as they are free
+  const int stride = ns * kAttnWaves;
+  for (; t < tiles; t += stride) {
+    const bool more = t + stride < tiles;
+    const uint8_t* tp = base + (size_t)(t + stride) * T.bytes();
 #pragma unroll
-    for (int j = 0; j < TileRegs<D>::VC; ++j)
-      *reinterpret_cast<u32x4*>(vl + v_chunk<D>(64 * j + lane)) = r.v[j];
+    for (int j = 0; j < VRegs<D, VPL>::VC; ++j)
+      *reinterpret_cast<u32x4*>(vl + v_chunk<D>(64 * j + lane)) = vr.v[j];
+    if (more) vr.load_codes(tp, lane);
     f32x4 s[NT][4];
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][kb] = f32x4{0, 0, 0, 0};
+      for (int kb = 0; kb < 4; ++kb) s[n][kb] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        const u32x4 a = k_operand<D>(r, kb, kt, ln.g);
+    for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        const u32x4 a = kr.operand(kb, kt, ln.g);
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[n][kb] = mfma16(a, q[n][kt], s[n][kb]);
       }
     }
-    float sv[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const uint32_t w = r.vs[j / 8][(j / 2) & 3];
-      sv[j] = __uint_as_float((j & 1) ? w & 0xffff0000u : w << 16);
-    }
+    if (more) kr.load(tp, ln);
     const bool edge = (t + 1) * kCacheTile > all;
     u32x4 pp[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int lim = last[n] - t * kCacheTile - 16 * ln.g;   // the row sees keys j <= lim
+      const int lim = last[n] - t * kCacheTile - key0;   // the row sees the lane's keys j <= lim
+      float x[VPL];
+      take_share<VPL>(s[n], ln.m, x);
       if (edge) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          s[n][j / 4][j & 3] = j <= lim ? s[n][j / 4][j & 3] : -kInf;
+        for (int j = 0; j < VPL; ++j) x[j] = j <= lim ? x[j] : -kInf;
       }
-      float mx = s[n][0][0];
+      float mx = x[0];
 #pragma unroll
-      for (int j = 1; j < 16; ++j) mx = __builtin_fmaxf(mx, s[n][j / 4][j & 3]);
+      for (int j = 1; j < VPL; ++j) mx = __builtin_fmaxf(mx, x[j]);
       if (__any(mx * p.sl2 > m2[n] + kLazy)) {
-        const float mt = max_quad(mx) * p.sl2;
+        const float mt = row_max<R::COLS>(mx) * p.sl2;
         const float mn = mt > m2[n] + kLazy ? mt : m2[n];
         const float alpha = mn == m2[n] ? 1.0f : __builtin_amdgcn_exp2f(m2[n] - mn);
         l[n] *= alpha;
@@ -541,21 +742,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
         m2[n] = mn;
       }
       const float nm = m2[n] == -kInf ? 0.f : -m2[n];
-      float pv[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][j / 4][j & 3], p.sl2, nm));
-        l[n] += x;
-        pv[j] = x * sv[j];
+      for (int j = 0; j < VPL; ++j) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], p.sl2, nm));
+        l[n] += e;
+        x[j] = e * vr.scale(j);
       }
       if (edge) {   // (the scales of keys that are not seen may be anything)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) pv[j] = j <= lim ? pv[j] : 0.f;
+        for (int j = 0; j < VPL; ++j) x[j] = j <= lim ? x[j] : 0.f;
       }
+      if constexpr (RP >= 16) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) pp[n][j / 4][j & 3] = pack_bf16x2(pv[2 * j], pv[2 * j + 1]);
+        for (int j = 0; j < 8; ++j) pp[n][j / 4][j & 3] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+      } else {
+        // 16 weights of a row and group in 32 bytes; every column reads its row's
+        uint8_t* a = pl + ((ln.m % RP) * 4 + ln.g) * 32;
+        uint8_t* w = a + (ln.m / RP) * VPL * 2;
+        if constexpr (VPL == 1) {
+          *reinterpret_cast<uint16_t*>(w) = (uint16_t)pack_bf16x2(x[0], 0.f);
+        } else if constexpr (VPL == 4) {
+          *reinterpret_cast<u32x2*>(w) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        } else {
+          *reinterpret_cast<u32x4*>(w) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                               pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+        }
+        pp[n][0] = *reinterpret_cast<const u32x4*>(a);
+        pp[n][1] = *reinterpret_cast<const u32x4*>(a + 16);
+      }
     }
-    u32x4 cs[2] = {r.cs[0], r.cs[1]};
+    u32x4 cs[2] = {vr.cs[0], vr.cs[1]};
     if ((t + 1) * kCacheTile > seen.len) {
       // sums of slots that were never written may be anything, NaN among it
       const int n = seen.len - t * kCacheTile - 16 * ln.g;
@@ -568,6 +784,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
       ck[n] = mfma16(cs[0], pp[n][0], ck[n]);
       ck[n] = mfma16(cs[1], pp[n][1], ck[n]);
     }
+    if (more) vr.load_scales(tp, key0, ln);
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
       // lane i of a group reads columns 16c .. of key 16g + i and gets column 16c + i
@@ -581,42 +798,26 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
         o[n][c] = mfma16(a1, pp[n][1], o[n][c]);
       }
     }
-  };
-
-  int t = split * tps + wave;
-  TileRegs<D> cur, nxt;
-  if (t < t_end) {
-    load_k<D>(cur, base + (size_t)t * T.bytes(), ln);
-    load_v<D>(cur, base + (size_t)t * T.bytes(), ln, lane);
-  }
-  for (; t < t_end; t += kAttnWaves) {
-    if (t + kAttnWaves < t_end) {
-      const uint8_t* tp = base + (size_t)(t + kAttnWaves) * T.bytes();
-      load_k<D>(nxt, tp, ln);
-      load_v<D>(nxt, tp, ln, lane);
-    }
-    step(t, cur);
-    cur = nxt;
   }
 
   // the waves' states: m = max_w m_w, x = sum_w x_w 2^(m_w - m), 16 rows at a time
   float* ex = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    l[n] = sum_quad(l[n]);
+    l[n] = row_sum<R::COLS>(l[n]);
     __syncthreads();   // the LDS is free
-    if (ln.g == 0) {
+    if (ln.m < R::COLS) {
       // hi and lo of c, and of c_w
-      st[wave][ln.m] = f32x4{m2[n], l[n], ck[n][0] + ck[n][1], ck[n][2] + ck[n][3]};
-    }
-    if (last[n] >= 0) {
+      if (ln.g == 0) st[wave][ln.m] = f32x4{m2[n], l[n], ck[n][0] + ck[n][1], ck[n][2] + ck[n][3]};
+      if (last[n] >= 0) {
 #pragma unroll
-      for (int c = 0; c < CB; ++c)
-        *reinterpret_cast<f32x4*>(ex + (wave * 16 + ln.m) * RS + 16 * c + 4 * ln.g) = o[n][c];
+        for (int c = 0; c < CB; ++c)
+          *reinterpret_cast<f32x4*>(ex + (wave * R::COLS + ln.m) * RS + 16 * c + 4 * ln.g) = o[n][c];
+      }
     }
     __syncthreads();
     constexpr int CPL = RowEnd<D>::CPL;
-    for (int i = wave; i < 16; i += kAttnWaves) {
+    for (int i = wave; i < R::COLS; i += kAttnWaves) {
       const int r = r0 + 16 * n + i;
       if (r >= p.R) break;   // wave-uniform, as all below
       const int lr = seen.last(p, r);
@@ -639,69 +840,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void cache_attn_
           if (lane < RowEnd<D>::LANES) {
 #pragma unroll
             for (int j = 0; j < CPL; ++j)
-              x[j] = __builtin_fmaf(f, ex[(w * 16 + i) * RS + CPL * lane + j], x[j]);
+              x[j] = __builtin_fmaf(f, ex[(w * R::COLS + i) * RS + CPL * lane + j], x[j]);
           }
         }
       }
-      if (p.nsplit == 1) {
+      if (ns == 1) {
         RowEnd<D>::run(p, row0 + r, lane, lr, x, mm, ls, cs, cw);
       } else {
+        // (to the memory that all XCDs see: their L2s are not coherent with each other)
         float* rec = p.ws + ((row0 + r) * p.nsplit + split) * RS;
-        if (lane == 0) *reinterpret_cast<f32x4*>(rec) = f32x4{mm, ls, cs, cw};
+        if (lane < 4) put(rec + lane, lane == 0 ? mm : lane == 1 ? ls : lane == 2 ? cs : cw);
         if (lane < RowEnd<D>::LANES) {
 #pragma unroll
-          for (int j = 0; j < CPL; ++j) rec[4 + CPL * lane + j] = x[j];
+          for (int j = 0; j < CPL; ++j) put(rec + 4 + CPL * lane + j, x[j]);
         }
       }
     }
   }
-}
-
-// ---- merge of the splits, one wave per row, as for the bf16 key split
-template <int D>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheParams p, int row_tile) {
-  constexpr int RS = D + 4, CPL = RowEnd<D>::CPL;
-  const int lane = threadIdx.x & 63;
-  const int nrb = (p.R + 3) / 4;
-  const int bh = blockIdx.x / nrb;
-  const int r = (blockIdx.x - bh * nrb) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (r >= p.R) return;
-  const Seen seen(p, bh / p.H);
-  const int keys = seen.keys(p, r / row_tile * row_tile, row_tile);
-  const int tiles = (keys + kCacheTile - 1) / kCacheTile;
-  const int tps = split_tiles(keys, p.nsplit);
-  const int ns = (tiles + tps - 1) / tps;   // the splits that ran
-  const size_t row = (size_t)bh * p.R + r;
-  const float* rec = p.ws + row * p.nsplit * RS;
-  f32x4 hd = {-kInf, 0.f, 0.f, 0.f};
-  if (lane < ns) hd = *reinterpret_cast<const f32x4*>(rec + (size_t)lane * RS);
-  constexpr int U = 8;   // splits whose outputs load together
-  float x[U][CPL], o[CPL];
-#pragma unroll
-  for (int j = 0; j < CPL; ++j) o[j] = 0.f;
-  auto load = [&](int s0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s0 + u < ns && lane < RowEnd<D>::LANES) {
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) x[u][j] = rec[(size_t)(s0 + u) * RS + 4 + CPL * lane + j];
-      }
-  };
-  load(0);
-  const float m = wave_max(hd[0]);
-  const float w = hd[0] == -kInf ? (nonfinite_bits(hd[1]) ? 1.f : 0.f) : __builtin_amdgcn_exp2f(hd[0] - m);
-  const float l = wave_sum(w * hd[1]), c = wave_sum(w * hd[2]), cw = wave_sum(w * hd[3]);
-  for (int s0 = 0; s0 < ns; s0 += U) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s0 + u < ns) {
-        const float f = __shfl(w, s0 + u);
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) o[j] = __builtin_fmaf(f, x[u][j], o[j]);
-      }
-    if (s0 + U < ns) load(s0 + U);
+  if (ns == 1) return;
+  // the last of the row tile's workgroups to come here merges the splits
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of the records is out
+  __syncthreads();
+  if (wave == 0) {
+    const bool is_last = last_to_arrive(p.tickets + ((size_t)bh * p.n_rt + rt) * p.nsplit, p.nonce, split,
+                                        ns, lane);
+    if (lane == 0) last_one = is_last;
   }
-  RowEnd<D>::run(p, row, lane, seen.last(p, r), o, m, l, c, cw);
+  __syncthreads();
+  if (!last_one) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");   // no older copy of a record is read
+  merge_splits<D>(p, seen, row0, r0, RP, ns, ex, st_w);
 }
 
 // ---- the keys' weights: weight_k <- decay * weight_k + sum over the head's rows of
@@ -721,8 +889,8 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
   const size_t row0 = (size_t)bh * p.R;
   const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
   for (int t = chunk * 4 + wave; t < tiles; t += chunks * 4) {
-    TileRegs<D> r;
-    load_k<D>(r, base + (size_t)t * T.bytes(), ln);
+    KRegs<D> r;
+    r.load(base + (size_t)t * T.bytes(), ln);
     float* wp = p.weight + ((size_t)bh * p.tiles + t) * kCacheTile + lane;
     const bool in = t * kCacheTile + lane < seen.len;
     const float old = in && p.decay != 0.f ? *wp : 0.f;
@@ -730,7 +898,7 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) a[kb][kt] = k_operand<D>(r, kb, kt, ln.g);
+      for (int kt = 0; kt < KT; ++kt) a[kb][kt] = r.operand(kb, kt, ln.g);
     float acc[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[j] = 0.f;
@@ -764,23 +932,23 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const bool hi = ln.m & 8;
-      const float keep = hi ? acc[j + 8] : acc[j], give = hi ? acc[j] : acc[j + 8];
+      const float keep = pick(hi, acc[j + 8], acc[j]), give = pick(hi, acc[j], acc[j + 8]);
       y[j] = keep + dpp<kXor15>(give);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool hi = ln.m & 4;
-      const float keep = hi ? y[j + 4] : y[j], give = hi ? y[j] : y[j + 4];
+      const float keep = pick(hi, y[j + 4], y[j]), give = pick(hi, y[j], y[j + 4]);
       z[j] = keep + dpp<kXor7>(give);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const bool hi = ln.m & 2;
-      const float keep = hi ? z[j + 2] : z[j], give = hi ? z[j] : z[j + 2];
+      const float keep = pick(hi, z[j + 2], z[j]), give = pick(hi, z[j], z[j + 2]);
       u[j] = keep + dpp<kXor3>(give);
     }
     const bool hi = ln.m & 1;
-    const float keep = hi ? u[1] : u[0], give = hi ? u[0] : u[1];
+    const float keep = pick(hi, u[1], u[0]), give = pick(hi, u[0], u[1]);
     const float sum = keep + dpp<kXor1>(give);
     if (in) *wp = p.decay != 0.f ? __builtin_fmaf(p.decay, old, sum) : sum;
   }
@@ -790,13 +958,14 @@ template <int D>
 int launch_attn(const CacheParams& p, hipStream_t s) {
   const int rt = cache_row_tile(p.R);
   const long long g = (long long)p.B * p.H * p.n_rt * p.nsplit;
-  const long long mg = (long long)p.B * p.H * ((p.R + 3) / 4);
-  if (g > INT_MAX || mg > INT_MAX) return -1;
+  if (g > INT_MAX) return -1;
   (void)hipGetLastError();
-  if (rt == 16) hipLaunchKernelGGL((cache_attn_kernel<D, 1>), dim3((unsigned)g), dim3(64 * kAttnWaves), 0, s, p);
-  else hipLaunchKernelGGL((cache_attn_kernel<D, 2>), dim3((unsigned)g), dim3(64 * kAttnWaves), 0, s, p);
-  if (p.nsplit > 1)
-    hipLaunchKernelGGL((cache_merge_kernel<D>), dim3((unsigned)mg), dim3(256), 0, s, p, rt);
+  const dim3 grid((unsigned)g), block(64 * kAttnWaves);
+  if (rt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, 1>), grid, block, 0, s, p);
+  else if (rt == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 4>), grid, block, 0, s, p);
+  else if (rt == 8) hipLaunchKernelGGL((cache_attn_kernel<D, 8>), grid, block, 0, s, p);
+  else if (rt == 16) hipLaunchKernelGGL((cache_attn_kernel<D, 16>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, 32>), grid, block, 0, s, p);
   if (p.weight) {
     // about four workgroups per CU, each wave one tile or more
     const long long heads = (long long)p.B * p.H;

@@ -34,8 +34,9 @@ def test_workspace_bytes():
     f = F.cache_workspace_bytes
     assert f(2, 3, 4, 5, 64, 1) == 0
     assert f(2, 3, 4, 5, 64, 1, True) == 2 * 3 * 4 * 5 * 16
-    assert f(2, 3, 4, 5, 64, 7) == 120 * 7 * 68 * 4
-    assert f(2, 3, 4, 5, 64, 7, True) == 120 * 7 * 68 * 4 + 120 * 16
+    # records of d + 4 floats, and 8 bytes for each head's row tile (20 rows: one), per split
+    assert f(2, 3, 4, 5, 64, 7) == 120 * 7 * 68 * 4 + 6 * 7 * 8
+    assert f(2, 3, 4, 5, 64, 7, True) == 120 * 7 * 68 * 4 + 120 * 16 + 6 * 7 * 8
     for args in ((0, 1, 1, 1, 64, 1), (1, 1, 1, 1, 64, 0), (1, 1, 1, 1, 64, 65), (1, 1, 0, 1, 64, 1),
                  (1 << 10, 1 << 10, 1 << 10, 2, 64, 1), (1, 1, 1, 1, 80, 1)):
         with pytest.raises(F.FabftError):
