@@ -12,6 +12,10 @@
 #include "fabft_cache.h"
 
 #include <climits>
+#include <type_traits>
+
+// v_mul_legacy_f32: the product, 0 if a factor is 0, whatever the other one is
+extern "C" __device__ __attribute__((const)) float mul_zero(float, float) __asm("llvm.amdgcn.fmul.legacy");
 
 namespace fabft {
 
@@ -267,9 +271,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRows p) {
 // of its query heads; rows i >= cnt are padding and see nothing.
 struct Seen {
   int len, cnt, off;   // causal: row i sees keys <= off + i
-  __device__ __forceinline__ Seen(const CacheParams& p, int b) {
-    len = clampi(p.lengths[b], 0, p.tiles * kCacheTile);
-    cnt = p.counts ? clampi(p.counts[b], 0, p.Lq) : p.Lq;
+  // lengths and counts: those of the sequence as loaded (without counts anything)
+  __device__ __forceinline__ Seen(const CacheParams& p, int lengths, int counts) {
+    // (in scalar registers, and all that follows from them)
+    len = clampi(__builtin_amdgcn_readfirstlane(lengths), 0, p.tiles * kCacheTile);
+    cnt = p.counts ? clampi(__builtin_amdgcn_readfirstlane(counts), 0, p.Lq) : p.Lq;
     off = len - cnt;
   }
   // the last key that row r sees, -1: none
@@ -644,14 +650,16 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
   const size_t row0 = (size_t)bh * p.R;
   const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
 
-  // the first tile loads before the lengths are known (every slot of the cache is memory)
+  // the lengths load first, so that nothing else has to arrive before they are used, and the
+  // first tile before they are known (every slot of the cache is memory)
+  const int len_b = p.lengths[b], cnt_b = p.counts ? p.counts[b] : 0;
   int t = split * kAttnWaves + wave;
   KRegs<D> kr;
   VRegs<D, VPL> vr;
-  if (t < p.tiles) {
-    const uint8_t* tp = base + (size_t)t * T.bytes();
-    kr.load(tp, ln);
+  {
+    const uint8_t* tp = base + (size_t)min(t, p.tiles - 1) * T.bytes();
     vr.load_codes(tp, lane);
+    kr.load(tp, ln);
     vr.load_scales(tp, key0, ln);
   }
   u32x4 q[NT][KT];
@@ -664,7 +672,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
     for (int kt = 0; kt < KT; ++kt)
       q[n][kt] = *reinterpret_cast<const u32x4*>(p.q + (row0 + r) * D + ln.g * (D / 4) + 8 * kt);
   }
-  const Seen seen(p, b);
+  const Seen seen(p, len_b, cnt_b);
   const int keys = seen.keys(p, r0, RP);
   const int tiles = (keys + kCacheTile - 1) / kCacheTile;
   const int ns = used_splits(tiles, p.nsplit);
@@ -693,15 +701,15 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
   uint8_t* vl = lds + wave * (VLDS + PLDS);
   uint8_t* pl = vl + VLDS;
 
-  // each part of the next tile loads into the registers of this one as soon as they are free
+  // One tile; with MORE each part of the wave's next one loads into the registers of this one
+  // as soon as they are free.
   const int stride = ns * kAttnWaves;
-  for (; t < tiles; t += stride) {
-    const bool more = t + stride < tiles;
+  auto step = [&](auto MORE) __attribute__((always_inline)) {
     const uint8_t* tp = base + (size_t)(t + stride) * T.bytes();
 #pragma unroll
     for (int j = 0; j < VRegs<D, VPL>::VC; ++j)
       *reinterpret_cast<u32x4*>(vl + v_chunk<D>(64 * j + lane)) = vr.v[j];
-    if (more) vr.load_codes(tp, lane);
+    if constexpr (MORE) vr.load_codes(tp, lane);
     f32x4 s[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -716,23 +724,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
         for (int n = 0; n < NT; ++n) s[n][kb] = mfma16(a, q[n][kt], s[n][kb]);
       }
     }
-    if (more) kr.load(tp, ln);
-    const bool edge = (t + 1) * kCacheTile > all;
-    u32x4 pp[NT][2];
+    if constexpr (MORE) kr.load(tp, ln);
+    float x[NT][VPL], mx[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) take_share<VPL>(s[n], ln.m, x[n]);
+    if ((t + 1) * kCacheTile > all) {
+      asm volatile("");   // a branch: most tiles pass it by, and selects would cost as much as the max
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int lim = last[n] - t * kCacheTile - key0;   // the row sees the lane's keys j <= lim
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) x[n][j] = j <= lim ? x[n][j] : -kInf;
+      }
+      // sums of slots that were never written may be anything, NaN among it
+      const int n = seen.len - t * kCacheTile - 16 * ln.g;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        vr.cs[j / 4][j & 3] &= (2 * j < n ? 0xffffu : 0u) | (2 * j + 1 < n ? 0xffff0000u : 0u);
+    }
+    bool far = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int lim = last[n] - t * kCacheTile - key0;   // the row sees the lane's keys j <= lim
-      float x[VPL];
-      take_share<VPL>(s[n], ln.m, x);
-      if (edge) {
+      mx[n] = x[n][0];
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) x[j] = j <= lim ? x[j] : -kInf;
-      }
-      float mx = x[0];
+      for (int j = 1; j < VPL; ++j) mx[n] = __builtin_fmaxf(mx[n], x[n][j]);
+      far = far || mx[n] * p.sl2 > m2[n] + kLazy;
+    }
+    if (__any(far)) {
 #pragma unroll
-      for (int j = 1; j < VPL; ++j) mx = __builtin_fmaxf(mx, x[j]);
-      if (__any(mx * p.sl2 > m2[n] + kLazy)) {
-        const float mt = row_max<R::COLS>(mx) * p.sl2;
+      for (int n = 0; n < NT; ++n) {
+        const float mt = row_max<R::COLS>(mx[n]) * p.sl2;
         const float mn = mt > m2[n] + kLazy ? mt : m2[n];
         const float alpha = mn == m2[n] ? 1.0f : __builtin_amdgcn_exp2f(m2[n] - mn);
         l[n] *= alpha;
@@ -741,64 +762,61 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
         for (int c = 0; c < CB; ++c) o[n][c] *= alpha;
         m2[n] = mn;
       }
+    }
+    u32x4 pp[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
       const float nm = m2[n] == -kInf ? 0.f : -m2[n];
 #pragma unroll
       for (int j = 0; j < VPL; ++j) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], p.sl2, nm));
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][j], p.sl2, nm));
         l[n] += e;
-        x[j] = e * vr.scale(j);
-      }
-      if (edge) {   // (the scales of keys that are not seen may be anything)
-#pragma unroll
-        for (int j = 0; j < VPL; ++j) x[j] = j <= lim ? x[j] : 0.f;
+        // 0 where e is 0, whatever the scale: that of a key that is not seen may be anything
+        x[n][j] = mul_zero(e, vr.scale(j));
       }
       if constexpr (RP >= 16) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pp[n][j / 4][j & 3] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+        for (int j = 0; j < 8; ++j) pp[n][j / 4][j & 3] = pack_bf16x2(x[n][2 * j], x[n][2 * j + 1]);
       } else {
         // 16 weights of a row and group in 32 bytes; every column reads its row's
         uint8_t* a = pl + ((ln.m % RP) * 4 + ln.g) * 32;
         uint8_t* w = a + (ln.m / RP) * VPL * 2;
         if constexpr (VPL == 1) {
-          *reinterpret_cast<uint16_t*>(w) = (uint16_t)pack_bf16x2(x[0], 0.f);
+          *reinterpret_cast<uint16_t*>(w) = (uint16_t)pack_bf16x2(x[n][0], 0.f);
         } else if constexpr (VPL == 4) {
-          *reinterpret_cast<u32x2*>(w) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+          *reinterpret_cast<u32x2*>(w) =
+              u32x2{pack_bf16x2(x[n][0], x[n][1]), pack_bf16x2(x[n][2], x[n][3])};
         } else {
-          *reinterpret_cast<u32x4*>(w) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                               pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+          *reinterpret_cast<u32x4*>(w) =
+              u32x4{pack_bf16x2(x[n][0], x[n][1]), pack_bf16x2(x[n][2], x[n][3]),
+                    pack_bf16x2(x[n][4], x[n][5]), pack_bf16x2(x[n][6], x[n][7])};
         }
         pp[n][0] = *reinterpret_cast<const u32x4*>(a);
         pp[n][1] = *reinterpret_cast<const u32x4*>(a + 16);
       }
     }
-    u32x4 cs[2] = {vr.cs[0], vr.cs[1]};
-    if ((t + 1) * kCacheTile > seen.len) {
-      // sums of slots that were never written may be anything, NaN among it
-      const int n = seen.len - t * kCacheTile - 16 * ln.g;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        cs[j / 4][j & 3] &= (2 * j < n ? 0xffffu : 0u) | (2 * j + 1 < n ? 0xffff0000u : 0u);
-    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      ck[n] = mfma16(cs[0], pp[n][0], ck[n]);
-      ck[n] = mfma16(cs[1], pp[n][1], ck[n]);
+      ck[n] = mfma16(vr.cs[0], pp[n][0], ck[n]);
+      ck[n] = mfma16(vr.cs[1], pp[n][1], ck[n]);
     }
-    if (more) vr.load_scales(tp, key0, ln);
+    if constexpr (MORE) vr.load_scales(tp, key0, ln);
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
       // lane i of a group reads columns 16c .. of key 16g + i and gets column 16c + i
       // of keys 16g .. 16g + 15
       const int a = v_chunk<D>((16 * ln.g + ln.m) * (D / 32) + c / 2) + 8 * (c & 1);
-      const i32x2 x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(vl + a));
-      const u32x4 a0 = decode8((uint32_t)x[0], 1.0f), a1 = decode8((uint32_t)x[1], 1.0f);
+      const i32x2 y = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(vl + a));
+      const u32x4 a0 = decode8((uint32_t)y[0], 1.0f), a1 = decode8((uint32_t)y[1], 1.0f);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         o[n][c] = mfma16(a0, pp[n][0], o[n][c]);
         o[n][c] = mfma16(a1, pp[n][1], o[n][c]);
       }
     }
-  }
+  };
+  for (; t + stride < tiles; t += stride) step(std::true_type{});
+  if (t < tiles) step(std::false_type{});
 
   // the waves' states: m = max_w m_w, x = sum_w x_w 2^(m_w - m), 16 rows at a time
   float* ex = reinterpret_cast<float*>(lds);
@@ -883,7 +901,8 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int bh = blockIdx.x / chunks, chunk = blockIdx.x - bh * chunks;
-  const Seen seen(p, bh / p.H);
+  const int b = bh / p.H;
+  const Seen seen(p, p.lengths[b], p.counts ? p.counts[b] : 0);
   const int tiles = (seen.len + kCacheTile - 1) / kCacheTile;
   const Lane<D> ln(lane, false);
   const size_t row0 = (size_t)bh * p.R;
