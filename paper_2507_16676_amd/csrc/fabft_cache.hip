@@ -1008,91 +1008,163 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 }
 
 constexpr int kEvictThreads = 1024;
+constexpr int kEvictKeys = 32;   // candidates in a thread's registers
+
+// An array in LDS that one wave scans, each lane C neighbours: a word of room every 32, so that
+// the lanes read different banks.
+__device__ __forceinline__ constexpr int skew(int i) { return i + i / 32; }
+
+// The bin (from the top, of N) in which the running count of a histogram reaches `need` >= 1,
+// and the count above it, by one wave.
+template <int N>
+__device__ __forceinline__ void find_bin(const int* hist, int need, int lane, int* bin, int* above) {
+  constexpr int C = N / 64;
+  int x[C], s = 0;
+#pragma unroll
+  for (int j = 0; j < C; ++j) s += x[j] = hist[skew(N - 1 - C * lane - j)];
+  int before = s;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(before, o);
+    if (lane >= o) before += y;
+  }
+  before -= s;
+  if (before < need && need <= before + s) {   // one lane
+    int at = N - 1 - C * lane, n = before;
+#pragma unroll
+    for (int j = 0; j < C - 1; ++j) {
+      const bool on = before + x[j] < need;   // (then for all before it too)
+      before += x[j];
+      if (on) n = before, --at;
+    }
+    *bin = at;
+    *above = n;
+  }
+}
 
 // One workgroup per head: the slots it keeps, in slot order. The last min(recent, len)
-// slots stay; of the others those with the largest weights, found as a threshold
-// by four passes over 8 bits of the weight each (a histogram of the candidates that
-// share the bits found so far); equal weights at the threshold go by slot.
-__global__ __launch_bounds__(kEvictThreads) void cache_select_kernel(CacheEvict p) {
-  __shared__ int hist[256];
-  __shared__ int wsum[2][kEvictThreads / 64];
-  __shared__ uint32_t sh_prefix;
-  __shared__ int sh_need;
+// slots stay; of the others those with the largest weights, found as a threshold by three
+// passes over 11, 11 and 10 bits of the weight (a histogram in LDS of the candidates that
+// share the bits found so far; 11 bits hold two of the mantissa, without which most weights
+// of a head would meet in a few bins); equal weights at the threshold go by slot. Up to
+// 32 candidates a thread are read once and stay in registers (with a load for each pass and
+// key, one after the other, 32,768 candidates took 71 us).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
+  constexpr int K = kEvictKeys, W = THREADS / 64, CHUNK = K * THREADS;
+  __shared__ int hist[skew(2048)];
+  __shared__ int cnt[2][skew(K * W) + 1];   // per row of 64 candidates: above the threshold, equal
+  __shared__ int sh_bin, sh_above;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bh = blockIdx.x, b = bh / p.H;
-  const int len = clampi(p.lengths[b], 0, p.tiles * kCacheTile);
+  const int len = clampi(__builtin_amdgcn_readfirstlane(p.lengths[b]), 0, p.tiles * kCacheTile);
   const int kept = min(len, p.keep);
   int* index = p.index + (size_t)bh * p.keep;
   if (tid == 0 && bh == b * p.H) p.new_lengths[b] = kept;
-  for (int j = kept + tid; j < p.keep; j += kEvictThreads) index[j] = -1;
+  for (int j = kept + tid; j < p.keep; j += THREADS) index[j] = -1;
   if (len <= p.keep) {
-    for (int j = tid; j < len; j += kEvictThreads) index[j] = j;
+    for (int j = tid; j < len; j += THREADS) index[j] = j;
     return;
   }
   const float* w = p.weight + (size_t)bh * p.tiles * kCacheTile;
   const int old = len - min(p.recent, p.keep);   // candidates: slots [0, old)
   const int want = kept - (len - old);           // of them to keep, < old
-  for (int j = tid; j < len - old; j += kEvictThreads) index[want + j] = old + j;
+  for (int j = tid; j < len - old; j += THREADS) index[want + j] = old + j;
   if (want <= 0) return;
+  uint32_t u[K];
+  auto load = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = c0 + k * THREADS;
+      u[k] = 0;
+      if (i + THREADS <= old) u[k] = __float_as_uint((w + i)[tid]);   // (the same for all)
+      else if (i + tid < old) u[k] = __float_as_uint((w + i)[tid]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (c0 + k * THREADS < old) u[k] = order_of(__uint_as_float(u[k]));
+    }
+  };
+  load(0);
   uint32_t prefix = 0;
   int need = want;   // how many of the candidates with the prefix to keep
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    for (int j = tid; j < skew(1 << bits); j += THREADS) hist[j] = 0;
     __syncthreads();
-    for (int i = tid; i < old; i += kEvictThreads) {
-      const uint32_t u = order_of(w[i]);
-      if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8)))
-        atomicAdd(&hist[(u >> shift) & 255], 1);
+    for (int c0 = 0; c0 < old; c0 += CHUNK) {
+      if (old > CHUNK) load(c0);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int i = c0 + k * THREADS;
+        if (i >= old) break;
+        if (i + tid < old && (pass == 0 || (u[k] >> (shift + bits)) == (prefix >> (shift + bits))))
+          atomicAdd(&hist[skew((u[k] >> shift) & ((1 << bits) - 1))], 1);
+      }
     }
     __syncthreads();
     if (wave == 0) {
-      // from the top: lane k has bins 255 - 4k .. 252 - 4k
-      int c[4], s = 0;
+      if (pass < 2) find_bin<2048>(hist, need, lane, &sh_bin, &sh_above);
+      else find_bin<1024>(hist, need, lane, &sh_bin, &sh_above);
+    }
+    __syncthreads();
+    prefix |= (uint32_t)sh_bin << shift;
+    need -= sh_above;
+  }
+  // prefix is the threshold: all above it, and the first `need` equal to it
+  const uint64_t below = (1ull << lane) - 1;
+  int ng0 = 0, ne0 = 0;   // of the chunks before
+  for (int c0 = 0; c0 < old; c0 += CHUNK) {
+    if (old > CHUNK) load(c0);
+    __syncthreads();
+    for (int j = tid; j < skew(K * W); j += THREADS) cnt[0][j] = cnt[1][j] = 0;
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s += c[j] = hist[255 - 4 * lane - j];
+    for (int k = 0; k < K; ++k) {
+      const int i = c0 + k * THREADS;
+      if (i >= old) break;
+      const bool in = i + tid < old;
+      const uint64_t mg = __ballot(in && u[k] > prefix), me = __ballot(in && u[k] == prefix);
+      if (lane == 0) {
+        cnt[0][skew(k * W + wave)] = __popcll(mg);
+        cnt[1][skew(k * W + wave)] = __popcll(me);
+      }
+    }
+    __syncthreads();
+    // running counts of the K * W rows: wave 0 the first kind, wave 1 the second
+    if (wave < 2) {
+      constexpr int C = K * W / 64;
+      int s = 0, x[C];
+#pragma unroll
+      for (int j = 0; j < C; ++j) s += x[j] = cnt[wave][skew(C * lane + j)];
       int before = s;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(before, o);
-        if (lane >= o) before += x;
+        const int y = __shfl_up(before, o);
+        if (lane >= o) before += y;
       }
+      if (lane == 63) cnt[wave][skew(K * W)] = before;
       before -= s;
-      if (before < need && need <= before + s) {   // one lane
-        int j = 0;
-        while (before + c[j] < need) before += c[j++];
-        sh_prefix = prefix | ((uint32_t)(255 - 4 * lane - j) << shift);
-        sh_need = need - before;
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        cnt[wave][skew(C * lane + j)] = before;
+        before += x[j];
       }
     }
     __syncthreads();
-    prefix = sh_prefix;
-    need = sh_need;
-  }
-  // prefix is the threshold: all above it, and the first `need` equal to it
-  int done_gt = 0, done_eq = 0;
-  for (int i0 = 0; i0 < old; i0 += kEvictThreads) {
-    const int i = i0 + tid;
-    const uint32_t u = i < old ? order_of(w[i]) : 0;
-    const bool gt = i < old && u > prefix, eq = i < old && u == prefix;
-    const uint64_t mg = __ballot(gt), me = __ballot(eq);
-    const uint64_t below = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) {
-      wsum[0][wave] = __popcll(mg);
-      wsum[1][wave] = __popcll(me);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = c0 + k * THREADS;
+      if (i >= old) break;
+      const bool in = i + tid < old, gt = in && u[k] > prefix, eq = in && u[k] == prefix;
+      const uint64_t mg = __ballot(gt), me = __ballot(eq);
+      const int ng = ng0 + cnt[0][skew(k * W + wave)] + __popcll(mg & below);
+      const int ne = ne0 + cnt[1][skew(k * W + wave)] + __popcll(me & below);
+      if (gt || (eq && ne < need)) index[ng + min(ne, need)] = i + tid;
     }
-    __syncthreads();
-    int ng = done_gt, ne = done_eq, tg = 0, te = 0;
-    for (int k = 0; k < kEvictThreads / 64; ++k) {
-      const int x = wsum[0][k], y = wsum[1][k];
-      if (k < wave) ng += x, ne += y;
-      tg += x, te += y;
-    }
-    ng += __popcll(mg & below);
-    ne += __popcll(me & below);
-    if (gt || (eq && ne < need)) index[ng + min(ne, need)] = i;
-    done_gt += tg;
-    done_eq += te;
+    ng0 += cnt[0][skew(K * W)];
+    ne0 += cnt[1][skew(K * W)];
   }
 }
 
@@ -1187,7 +1259,11 @@ int launch_evict(const CacheEvict& p, hipStream_t s) {
   const int batches = p.into == p.cache ? 1 : (p.keep + 1023) / 1024;
   if (heads > INT_MAX || heads * batches * 2 > INT_MAX) return -1;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)heads), dim3(kEvictThreads), 0, s, p);
+  // four waves meet sooner than sixteen, as long as they hold the candidates
+  if (p.tiles * kCacheTile <= 256 * kEvictKeys)
+    hipLaunchKernelGGL((cache_select_kernel<256>), dim3((unsigned)heads), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((cache_select_kernel<1024>), dim3((unsigned)heads), dim3(1024), 0, s, p);
   hipLaunchKernelGGL((cache_move_kernel<D>), dim3((unsigned)(heads * batches * 2)),
                      dim3(kEvictThreads), 0, s, p, batches);
   return hipGetLastError() == hipSuccess ? 0 : -1;
