@@ -89,11 +89,14 @@ struct CacheEvict {
 
 // Query rows of a workgroup of the attention, for R rows per key/value head.
 inline int cache_row_tile(int R) { return R <= 1 ? 1 : R <= 4 ? 4 : R <= 8 ? 8 : R <= 16 ? 16 : 32; }
+// As many tiles stay with one workgroup: a merge costs 2.2 us, a round of tiles 0.9.
+constexpr int kCacheFewTiles = 12;
 // Splits of the keys of a cache of `tiles` tiles: two workgroups per CU (512) while each has 16
 // tiles or more, four for each of its waves, else one per CU. Measured (us, splits at 512 and
 // at 256 workgroups): 128 heads of 512 tiles 109 113, 64 of 512 30.0 33.4, 128 of 128 30.8
 // 32.0; 32 heads of 65 tiles 13.1 11.8, 64 of 32 13.1 12.7, 8 heads of 512 21.6 18.4.
 inline int cache_splits(int B, int H, int R, int tiles) {
+  if (tiles <= kCacheFewTiles) return 1;
   const long long units = (long long)B * H * ((R + cache_row_tile(R) - 1) / cache_row_tile(R));
   long long ns = (512 + units - 1) / units;
   if (tiles < 16 * ns) ns = (256 + units - 1) / units;

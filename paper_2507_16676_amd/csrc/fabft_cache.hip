@@ -11,6 +11,7 @@
 // the check of the rows that see it.
 #include "fabft_cache.h"
 
+#include <algorithm>
 #include <climits>
 #include <type_traits>
 
@@ -504,10 +505,9 @@ __device__ __forceinline__ float row_max(float x) {
 
 constexpr int kAttnWaves = 4;
 
-// The splits of a row tile that sees `tiles` tiles: each wave has a tile, and a few tiles stay
-// with one workgroup (a merge costs 2.2 us, a round of tiles 0.9).
+// The splits of a row tile that sees `tiles` tiles: each wave has a tile.
 __device__ __forceinline__ int used_splits(int tiles, int nsplit) {
-  return tiles <= 3 * kAttnWaves ? 1 : min(nsplit, (tiles + kAttnWaves - 1) / kAttnWaves);
+  return tiles <= kCacheFewTiles ? 1 : min(nsplit, (tiles + kAttnWaves - 1) / kAttnWaves);
 }
 
 __device__ __forceinline__ void put(float* a, float x) {
@@ -539,11 +539,28 @@ __device__ __forceinline__ bool last_to_arrive(unsigned long long* words, unsign
   return true;
 }
 
+// Four columns of a row over the splits, U of them at a time; w: the splits' weights.
+template <int U>
+__device__ __forceinline__ f32x4 merge_columns(const float* a, size_t step, int ns, const float* w) {
+  f32x4 o = {0, 0, 0, 0};
+  for (int s0 = 0; s0 < ns; s0 += U) {
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4*>(a + min(s0 + u, ns - 1) * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = s0 + u < ns ? w[s0 + u] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = s0 + u < ns ? __builtin_fmaf(f, x[u][j], o[j]) : o[j];
+    }
+  }
+  return o;
+}
+
 // The splits' records of the workgroup's rows: m = max_s m_s, x = sum_s x_s 2^(m_s - m) for x in
-// {l, o, c, c_w} (c merges like one more column of o, Eq. 10), then the rows' ends. A chain of
-// memory latencies: the heads of all records load together with the first columns (the
-// splits' weights go to st_w), and a thread takes four columns of a row over the splits,
-// eight at a time.
+// {l, o, c, c_w} (c merges like one more column of o, Eq. 10), then the rows' ends. One
+// workgroup reads all records from beyond its L2, so what counts is how many loads it has in
+// flight: a thread takes four columns of a row over up to 32 splits at once.
 template <int D>
 __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& seen, size_t row0, int r0,
                                              int rows_most, int ns, float* ex, float* st_w) {
@@ -553,7 +570,7 @@ __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& s
   for (int b0 = 0; b0 < rows; b0 += 16) {   // 16 rows at a time
     const int nr = min(16, rows - b0);
     const float* rec = p.ws + (row0 + r0 + b0) * p.nsplit * RS;
-    f32x4 h[K], x[8];
+    f32x4 h[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int i = wave + W * k;
@@ -561,14 +578,6 @@ __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& s
       if (i < nr && lane < ns)
         h[k] = *reinterpret_cast<const f32x4*>(rec + ((size_t)i * p.nsplit + lane) * RS);
     }
-    auto load = [&](int e, int s0) __attribute__((always_inline)) {
-      const int i = e / C4;
-      const float* a = rec + (size_t)i * p.nsplit * RS + 4 + 4 * (e - i * C4);
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        x[u] = *reinterpret_cast<const f32x4*>(a + (size_t)min(s0 + u, ns - 1) * RS);
-    };
-    if (tid < nr * C4) load(tid, 0);
     float m[K], l[K], c[K], cw[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -583,19 +592,9 @@ __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& s
     __syncthreads();
     for (int e = tid; e < nr * C4; e += 64 * W) {
       const int i = e / C4;
-      f32x4 o = {0, 0, 0, 0};
-      for (int s0 = 0; s0 < ns; s0 += 8) {
-        if (e != tid || s0 > 0) load(e, s0);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          if (s0 + u < ns) {
-            const float w = st_w[i * 64 + s0 + u];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(w, x[u][j], o[j]);
-          }
-        }
-      }
-      *reinterpret_cast<f32x4*>(ex + i * RS + 4 * (e - i * C4)) = o;
+      const float* a = rec + (size_t)i * p.nsplit * RS + 4 + 4 * (e - i * C4);
+      *reinterpret_cast<f32x4*>(ex + i * RS + 4 * (e - i * C4)) =
+          ns <= 8 ? merge_columns<8>(a, RS, ns, st_w + i * 64) : merge_columns<32>(a, RS, ns, st_w + i * 64);
     }
     __syncthreads();
 #pragma unroll
@@ -875,7 +874,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
       }
     }
   }
-  if (ns == 1) return;
+  if (ns == 1 || !p.tickets) return;
   // the last of the row tile's workgroups to come here merges the splits
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of the records is out
   __syncthreads();
@@ -888,6 +887,38 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
   if (!last_one) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");   // no older copy of a record is read
   merge_splits<D>(p, seen, row0, r0, RP, ns, ex, st_w);
+}
+
+// The same merge as a launch of its own, one wave per row, for records that are too much for
+// one workgroup per row tile (launch_attn says when).
+template <int D>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheParams p, int row_tile) {
+  constexpr int RS = D + 4, CPL = RowEnd<D>::CPL;
+  __shared__ float st_w[4][64];
+  __shared__ __align__(16) float ex[4][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nrb = (p.R + 3) / 4;
+  const int bh = blockIdx.x / nrb, b = bh / p.H;
+  const int r = (blockIdx.x - bh * nrb) * 4 + wave;
+  if (r >= p.R) return;   // (the waves do not meet)
+  const Seen seen(p, p.lengths[b], p.counts ? p.counts[b] : 0);
+  const int tiles = (seen.keys(p, r / row_tile * row_tile, row_tile) + kCacheTile - 1) / kCacheTile;
+  const int ns = used_splits(tiles, p.nsplit);
+  if (ns == 1) return;   // the row is done
+  const size_t row = (size_t)bh * p.R + r;
+  const float* rec = p.ws + row * p.nsplit * RS;
+  f32x4 h = {-kInf, 0.f, 0.f, 0.f};
+  if (lane < ns) h = *reinterpret_cast<const f32x4*>(rec + (size_t)lane * RS);
+  const float m = wave_max(h[0]);
+  const float w = h[0] == -kInf ? (nonfinite_bits(h[1]) ? 1.f : 0.f) : __builtin_amdgcn_exp2f(h[0] - m);
+  const float l = wave_sum(w * h[1]), c = wave_sum(w * h[2]), cw = wave_sum(w * h[3]);
+  st_w[wave][lane] = w;
+  if (lane < D / 4)
+    *reinterpret_cast<f32x4*>(&ex[wave][4 * lane]) = merge_columns<32>(rec + 4 + 4 * lane, RS, ns, st_w[wave]);
+  float y[CPL];
+#pragma unroll
+  for (int j = 0; j < CPL; ++j) y[j] = lane < RowEnd<D>::LANES ? ex[wave][CPL * lane + j] : 0.f;
+  RowEnd<D>::run(p, row, lane, seen.last(p, r), y, m, l, c, cw);
 }
 
 // ---- the keys' weights: weight_k <- decay * weight_k + sum over the head's rows of
@@ -974,17 +1005,25 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
 }
 
 template <int D>
-int launch_attn(const CacheParams& p, hipStream_t s) {
-  const int rt = cache_row_tile(p.R);
-  const long long g = (long long)p.B * p.H * p.n_rt * p.nsplit;
-  if (g > INT_MAX) return -1;
+int launch_attn(const CacheParams& p0, hipStream_t s) {
+  const int rt = cache_row_tile(p0.R);
+  const long long g = (long long)p0.B * p0.H * p0.n_rt * p0.nsplit;
+  const long long mg = (long long)p0.B * p0.H * ((p0.R + 3) / 4);
+  if (g > INT_MAX || mg > INT_MAX) return -1;
   (void)hipGetLastError();
   const dim3 grid((unsigned)g), block(64 * kAttnWaves);
+  // One CU takes 60 GB/s or so from beyond its L2: 16 rows of 256 over 32 splits, 530 KB of
+  // records a row tile, took 14 us of 32 in the last workgroup, and 8 as a launch of its own; 33 KB
+  // (one row of 128, 64 splits) 5 and 7.
+  const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 200000;
+  CacheParams p = p0;
+  if (apart) p.tickets = nullptr;
   if (rt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, 1>), grid, block, 0, s, p);
   else if (rt == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 4>), grid, block, 0, s, p);
   else if (rt == 8) hipLaunchKernelGGL((cache_attn_kernel<D, 8>), grid, block, 0, s, p);
   else if (rt == 16) hipLaunchKernelGGL((cache_attn_kernel<D, 16>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((cache_attn_kernel<D, 32>), grid, block, 0, s, p);
+  if (apart) hipLaunchKernelGGL((cache_merge_kernel<D>), dim3((unsigned)mg), dim3(256), 0, s, p, rt);
   if (p.weight) {
     // about four workgroups per CU, each wave one tile or more
     const long long heads = (long long)p.B * p.H;
@@ -1052,7 +1091,7 @@ __device__ __forceinline__ void find_bin(const int* hist, int need, int lane, in
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
   constexpr int K = kEvictKeys, W = THREADS / 64, CHUNK = K * THREADS;
-  __shared__ int hist[skew(2048)];
+  __shared__ int hists[3][skew(2048)];
   __shared__ int cnt[2][skew(K * W) + 1];   // per row of 64 candidates: above the threshold, equal
   __shared__ int sh_bin, sh_above;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -1071,6 +1110,7 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
   const int want = kept - (len - old);           // of them to keep, < old
   for (int j = tid; j < len - old; j += THREADS) index[want + j] = old + j;
   if (want <= 0) return;
+  for (int j = tid; j < 3 * skew(2048); j += THREADS) hists[0][j] = 0;
   uint32_t u[K];
   auto load = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
@@ -1091,8 +1131,8 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int j = tid; j < skew(1 << bits); j += THREADS) hist[j] = 0;
-    __syncthreads();
+    int* hist = hists[pass];
+    if (pass == 0) __syncthreads();
     for (int c0 = 0; c0 < old; c0 += CHUNK) {
       if (old > CHUNK) load(c0);
 #pragma unroll
