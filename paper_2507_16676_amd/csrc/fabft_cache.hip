@@ -29,6 +29,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
@@ -52,6 +53,11 @@ __device__ __forceinline__ u32x4 decode8(uint32_t x, float scale) {
   r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2));
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
   return r;
+}
+// a.lo*b.lo + a.hi*b.hi + c on bf16 pairs
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c,
+                                         false);
 }
 // 2^(e - 127) from byte i of x; 255: infinity
 __device__ __forceinline__ float scale_of_byte(uint32_t x, int i) {
@@ -126,13 +132,13 @@ __device__ __forceinline__ uint32_t span_max(uint32_t x) {
   return x;
 }
 __device__ __forceinline__ uint32_t max_abs8(u32x4 x) {   // of eight bf16, as bits
-  uint32_t m = 0;
+  u16x2 m = __builtin_bit_cast(u16x2, x[0] & 0x7fff7fffu);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m = max(m, x[i] & 0x7fffu);
-    m = max(m, (x[i] >> 16) & 0x7fffu);
+  for (int i = 1; i < 4; ++i) {
+    const uint32_t y = x[i] & 0x7fff7fffu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, y));
   }
-  return m;
+  return max((uint32_t)m[0], (uint32_t)m[1]);
 }
 
 // Lanes of a row of D channels, eight each; 96 channels take 12 of 16 lanes.
@@ -145,26 +151,9 @@ struct RowLanes {
 // ---- append: one row of K and of V per RowLanes<D>::N lanes. Moves 4d bytes in and
 // about d + 14 out per row: bound by memory with many rows, by latency with few.
 template <int D>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
+__device__ __forceinline__ void append_row(uint8_t* tile, int key, int lane, bool live, u32x4 k, u32x4 v) {
   constexpr int N = RowLanes<D>::N;
   constexpr CacheTile T(D);
-  const int lane = threadIdx.x % N;
-  const long long row = (long long)blockIdx.x * RowLanes<D>::ROWS + threadIdx.x / N;
-  const long long bh = row / p.n;
-  const int i = (int)(row - bh * p.n);
-  if (bh >= (long long)p.B * p.H) return;   // whole groups of N lanes leave together
-  const int b = (int)(bh / p.H), h = (int)(bh - (long long)b * p.H);
-  const long long slot = (long long)p.start[b] + i;
-  if ((p.counts && i >= p.counts[b]) || slot < 0 || slot >= (long long)p.tiles * kCacheTile) return;
-  const bool live = lane < D / 8;
-  u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-  if (live) {
-    k = *reinterpret_cast<const u32x4*>(p.k + b * p.kb + h * p.kh + i * p.kn + 8 * lane);
-    v = *reinterpret_cast<const u32x4*>(p.v + b * p.vb + h * p.vh + i * p.vn + 8 * lane);
-  }
-  uint8_t* tile = p.cache + (bh * p.tiles + slot / kCacheTile) * T.bytes();
-  const int key = (int)(slot % kCacheTile);
-
   // K: 2^e, the smallest with max < 7 * 2^e: m 2^x with m < 1.75 gives x - 2, else x - 1
   const uint32_t ka = span_max<4>(max_abs8(k));
   const bool kbad = ka >= 0x7f80u;
@@ -183,22 +172,22 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
     if (kbad) kc = 0;
   }
 
-  // V: s, the smallest number of six significant bits >= max / 6. max has eight bits, so
-  // a quotient that is no such number is 2^-10 or more away from the next one: the
-  // rounding of the division does not change s
+  // V: s, the smallest number of six significant bits >= max / 6. max has eight bits, so a
+  // quotient that is no such number is 2^-10 or more away from one: taken 2^-20 too small, a
+  // quotient that is one does not move up to the next, and no other one changes
   const uint32_t va = span_max<N>(max_abs8(v));
   const bool vbad = va >= 0x7f80u;
-  float s = __builtin_fmaxf(__uint_as_float(va << 16) / 6.0f, 0x1p-100f);
+  float s = __builtin_fmaxf(__uint_as_float(va << 16) * 0x1.55554p-3f, 0x1p-100f);
   s = __uint_as_float((__float_as_uint(s) + 0x3ffffu) & ~0x3ffffu);
   s = __builtin_fminf(s, 0x1.5p+125f);   // (6 s is a bf16 number)
   if (vbad) s = 1.0f;
-  const float rs = 1.0f / s;
+  const float rs = __builtin_amdgcn_rcpf(s);
   uint32_t vc = 0;
   float sum = 0.f, wsum = 0.f;
   {
     // x / s in fp16: x and c s (c a border between codes) have at most 9 bits, so a
     // quotient is a border itself or at least 2^-9 of it away, and x * (1 / s), off by
-    // 2^-23, rounds to the border or to its right side
+    // 2^-22, rounds to the border or to its right side
     uint32_t hp[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -214,9 +203,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
     const u32x4 x = decode8(vc, 1.0f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float even = __uint_as_float(x[j] << 16), odd = __uint_as_float(x[j] & 0xffff0000u);
-      sum += even + odd;
-      wsum += even - odd;
+      sum = dot2(x[j], 0x3f803f80u, sum);      // (1, 1)
+      wsum = dot2(x[j], 0xbf803f80u, wsum);    // (1, -1)
     }
     sum = span_sum<N>(sum);     // multiples of 1/2 up to 1536: exact
     wsum = span_sum<N>(wsum);
@@ -232,6 +220,53 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
     const float y = lane == 0 ? s : (lane & 1) ? hi : x - hi;
     const uint16_t u = lane == 0 && vbad ? (uint16_t)0x7fc0 : (uint16_t)(__float_as_uint(y) >> 16);
     *reinterpret_cast<uint16_t*>(tile + T.vscale() + lane * 2 * kCacheTile + 2 * key) = u;
+  }
+}
+
+// ITER passes over ROWS rows. Many rows: a workgroup takes 64 neighbours of one head, all
+// their loads first, so that it alone writes most lines of the scales and sums (their rows of
+// 2 and 4 bytes; lines that several XCDs write in parts cost more) and has more on its way.
+// (4 x 32 heads, 4,096 rows of 128: 80 us with 16 rows a workgroup and a division for s and
+// 1 / s each, 65 now: 5.3 TB/s, the rate of a large copy.)
+template <int D, int ITER>
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
+  constexpr int N = RowLanes<D>::N, ROWS = RowLanes<D>::ROWS;
+  constexpr CacheTile T(D);
+  const int lane = threadIdx.x % N, sub = threadIdx.x / N;
+  const bool live = lane < D / 8;
+  long long bh;
+  int i0;
+  if constexpr (ITER > 1) {
+    const int chunks = (p.n + ITER * ROWS - 1) / (ITER * ROWS);
+    bh = blockIdx.x / chunks;
+    i0 = (int)(blockIdx.x - bh * chunks) * ITER * ROWS + sub;
+  } else {
+    const long long row = (long long)blockIdx.x * ROWS + sub;
+    bh = row / p.n;
+    i0 = (int)(row - bh * p.n);
+  }
+  if (bh >= (long long)p.B * p.H) return;   // whole groups of N lanes leave together
+  const int b = (int)(bh / p.H), h = (int)(bh - (long long)b * p.H);
+  const int start = p.start[b], slots = p.tiles * kCacheTile;   // (at most 2^30)
+  const int n = p.counts ? min(p.n, p.counts[b]) : p.n;
+  uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
+  u32x4 k[ITER], v[ITER];
+#pragma unroll
+  for (int it = 0; it < ITER; ++it) {
+    const int i = i0 + it * ROWS;
+    k[it] = v[it] = u32x4{0, 0, 0, 0};
+    if (live && i < n) {
+      k[it] = *reinterpret_cast<const u32x4*>(p.k + b * p.kb + h * p.kh + i * p.kn + 8 * lane);
+      v[it] = *reinterpret_cast<const u32x4*>(p.v + b * p.vb + h * p.vh + i * p.vn + 8 * lane);
+    }
+  }
+#pragma unroll
+  for (int it = 0; it < ITER; ++it) {
+    const int i = i0 + it * ROWS;
+    const uint32_t slot = (uint32_t)start + (uint32_t)i;   // (one before 0 is past the end)
+    if (i < n && slot < (uint32_t)slots)
+      append_row<D>(base + (size_t)(slot / kCacheTile) * T.bytes(), (int)(slot % kCacheTile), lane, live,
+                    k[it], v[it]);
   }
 }
 
@@ -922,25 +957,63 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheParams p, int row
 }
 
 // ---- the keys' weights: weight_k <- decay * weight_k + sum over the head's rows of
-// 2^(s - m) / l, with the m and l of the finished rows. A second product K Q^T; every key
-// belongs to one wave, so the sums have one order. The scores are those of the
-// attention, bit for bit.
-template <int D>
+// 2^(s - m) / l, with the m and l of the finished rows. A second product K Q^T (the scores of
+// the attention, bit for bit); every key belongs to one wave, so the sums have one order.
+// K turns into operands once per tile, the rows go by 16 at a time. More than 16 rows lie in
+// LDS, 128 of them at once, for the four waves (each with its tile); loaded by every wave
+// from the L2, one operand ahead, 128 rows took twice as long. What bounds it then is the
+// exponentials.
+constexpr int kWeightRows = 128;   // of q in LDS
+
+template <int D, bool MANY>
 __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int chunks) {
   constexpr CacheTile T(D);
   constexpr int KT = D / 32;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int QS = 2 * D + 16;   // bytes of a row in LDS (the rows in different banks)
+  __shared__ __align__(16) uint8_t lq[MANY ? kWeightRows * QS : 16];
+  __shared__ f32x4 lst[MANY ? kWeightRows : 1];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x / chunks, chunk = blockIdx.x - bh * chunks;
   const int b = bh / p.H;
-  const Seen seen(p, p.lengths[b], p.counts ? p.counts[b] : 0);
-  const int tiles = (seen.len + kCacheTile - 1) / kCacheTile;
   const Lane<D> ln(lane, false);
   const size_t row0 = (size_t)bh * p.R;
   const uint8_t* base = p.cache + (size_t)bh * p.tiles * T.bytes();
-  for (int t = chunk * 4 + wave; t < tiles; t += chunks * 4) {
-    KRegs<D> r;
-    r.load(base + (size_t)t * T.bytes(), ln);
+  const int len_b = p.lengths[b], cnt_b = p.counts ? p.counts[b] : 0;
+  int t = chunk * 4 + wave;
+  KRegs<D> r;
+  r.load(base + (size_t)min(t, p.tiles - 1) * T.bytes(), ln);
+  // rows c0 .. of q and their m, 1 / l: to LDS, by all
+  auto stage = [&](int c0) __attribute__((always_inline)) {
+    const int n = min(kWeightRows, p.R - c0);
+    for (int e = tid; e < n * (D / 8); e += 256) {
+      const int i = e / (D / 8), c = e - i * (D / 8);
+      *reinterpret_cast<u32x4*>(lq + i * QS + 16 * c) =
+          *reinterpret_cast<const u32x4*>(p.q + (row0 + c0 + i) * D + 8 * c);
+    }
+    if (tid < n) lst[tid] = *reinterpret_cast<const f32x4*>(p.stats + 4 * (row0 + c0 + tid));
+  };
+  u32x4 q1[KT];
+  f32x4 st1;
+  if constexpr (MANY) {
+    stage(0);
+    __syncthreads();
+  } else {
+    const size_t row = row0 + min(ln.m, p.R - 1);
+    st1 = *reinterpret_cast<const f32x4*>(p.stats + 4 * row);
+    if (ln.m >= p.R) st1[1] = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+      // (rows that add nothing: their q may hold anything)
+      q1[kt] = st1[1] > 0.f ? *reinterpret_cast<const u32x4*>(p.q + row * D + ln.g * (D / 4) + 8 * kt)
+                            : u32x4{0, 0, 0, 0};
+  }
+  const Seen seen(p, len_b, cnt_b);
+  const int tiles = (seen.len + kCacheTile - 1) / kCacheTile;
+  // (the waves of a workgroup go round together, with or without a tile: they meet at the LDS)
+  for (; t - wave < tiles; t += chunks * 4) {
+    const bool work = t < tiles;
+    if (!MANY && !work) break;
     float* wp = p.weight + ((size_t)bh * p.tiles + t) * kCacheTile + lane;
     const bool in = t * kCacheTile + lane < seen.len;
     const float old = in && p.decay != 0.f ? *wp : 0.f;
@@ -949,32 +1022,62 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) a[kb][kt] = r.operand(kb, kt, ln.g);
+    const int tn = t + chunks * 4;
+    if (tn < tiles) r.load(base + (size_t)tn * T.bytes(), ln);
+    // keys that some row that sees any does not see
+    const bool edge = (t + 1) * kCacheTile > (p.causal ? seen.off + 1 : seen.len);
     float acc[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-    for (int r0 = 0; r0 < p.R; r0 += 16) {
-      const int row = r0 + ln.m;
-      u32x4 q[KT];
-      f32x4 st = {kInf, 0.f, __int_as_float(-1), 0.f};
-      if (row < p.R) st = *reinterpret_cast<const f32x4*>(p.stats + 4 * (row0 + row));
-      const int lim = __float_as_int(st[2]) - t * kCacheTile - 16 * ln.g;
+    auto rows16 = [&](const u32x4 (&q)[KT], const f32x4& st) __attribute__((always_inline)) {
+      f32x4 s[4];
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        q[kt] = u32x4{0, 0, 0, 0};
-        if (row < p.R)
-          q[kt] = *reinterpret_cast<const u32x4*>(p.q + (row0 + row) * D + ln.g * (D / 4) + 8 * kt);
+      for (int kb = 0; kb < 4; ++kb) s[kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) s[kb] = mfma16(a[kb][kt], q[kt], s[kb]);
+      if (edge) {
+        asm volatile("");   // (a branch)
+        const int lim = __float_as_int(st[2]) - t * kCacheTile - 16 * ln.g;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j / 4][j & 3] = j <= lim ? s[j / 4][j & 3] : -kInf;
       }
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        f32x4 s = {0, 0, 0, 0};
+      for (int j = 0; j < 16; ++j)
+        acc[j] = __builtin_fmaf(
+            __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j & 3], p.sl2, -st[0])), st[1], acc[j]);
+    };
+    if constexpr (!MANY) {
+      rows16(q1, st1);
+    } else {
+      for (int c0 = 0; c0 < p.R; c0 += kWeightRows) {
+        if (p.R > kWeightRows) {
+          __syncthreads();
+          stage(c0);
+          __syncthreads();
+        }
+        if (!work) continue;
+        const int n = min(kWeightRows, p.R - c0);
+        for (int r0 = 0; r0 < n; r0 += 16) {
+          const int i = min(r0 + ln.m, n - 1);
+          f32x4 st = lst[i];
+          if (r0 + ln.m >= n) st[1] = 0.f;
+          u32x4 q[KT];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) s = mfma16(a[kb][kt], q[kt], s);
+          for (int kt = 0; kt < KT; ++kt)
+            q[kt] = *reinterpret_cast<const u32x4*>(lq + i * QS + ln.g * (D / 2) + 16 * kt);
+          if (__any(!(st[1] > 0.f))) {
+            asm volatile("");   // (a branch) rows that add nothing: their q may hold anything
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.sl2, -st[0])) * st[1];
-          acc[4 * kb + i] += 4 * kb + i <= lim ? x : 0.f;
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) q[kt][e] = st[1] > 0.f ? q[kt][e] : 0;
+          }
+          rows16(q, st);
         }
       }
+      if (!work) continue;
     }
     // sum over the 16 rows (lanes n) with half the values left after each step: lane n
     // ends with key 16g + n
@@ -1031,7 +1134,9 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
     long long ch = (1024 + heads - 1) / heads;
     if (ch > most) ch = most;
     if (heads * ch > INT_MAX) return -1;
-    hipLaunchKernelGGL((cache_weight_kernel<D>), dim3((unsigned)(heads * ch)), dim3(256), 0, s, p, (int)ch);
+    const dim3 wg((unsigned)(heads * ch));
+    if (p.R > 16) hipLaunchKernelGGL((cache_weight_kernel<D, true>), wg, dim3(256), 0, s, p, (int)ch);
+    else hipLaunchKernelGGL((cache_weight_kernel<D, false>), wg, dim3(256), 0, s, p, (int)ch);
   }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
@@ -1310,25 +1415,37 @@ int launch_evict(const CacheEvict& p, hipStream_t s) {
 }
 
 template <int D>
-int launch_rows(const CacheRows& p, bool append, hipStream_t s) {
+int launch_append(const CacheRows& p, hipStream_t s) {
+  constexpr int ROWS = RowLanes<D>::ROWS, ITER = 64 / ROWS;
+  const long long heads = (long long)p.B * p.H;
+  const bool many = p.n >= 64;
+  const long long g = many ? heads * ((p.n + 63) / 64) : (heads * p.n + ROWS - 1) / ROWS;
+  if (g > INT_MAX) return -1;
+  (void)hipGetLastError();
+  if (many) hipLaunchKernelGGL((cache_append_kernel<D, ITER>), dim3((unsigned)g), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((cache_append_kernel<D, 1>), dim3((unsigned)g), dim3(256), 0, s, p);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+template <int D>
+int launch_read(const CacheRows& p, hipStream_t s) {
   const long long rows = (long long)p.B * p.H * p.n;
   const long long g = (rows + RowLanes<D>::ROWS - 1) / RowLanes<D>::ROWS;
   if (g > INT_MAX) return -1;
   (void)hipGetLastError();
-  if (append) hipLaunchKernelGGL((cache_append_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((cache_read_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((cache_read_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 }  // namespace
 
 int launch_cache_append(const CacheRows& p, int d, hipStream_t s) {
-  return d == 64 ? launch_rows<64>(p, true, s) : d == 96 ? launch_rows<96>(p, true, s)
-       : d == 128 ? launch_rows<128>(p, true, s) : launch_rows<256>(p, true, s);
+  return d == 64 ? launch_append<64>(p, s) : d == 96 ? launch_append<96>(p, s)
+       : d == 128 ? launch_append<128>(p, s) : launch_append<256>(p, s);
 }
 int launch_cache_read(const CacheRows& p, int d, hipStream_t s) {
-  return d == 64 ? launch_rows<64>(p, false, s) : d == 96 ? launch_rows<96>(p, false, s)
-       : d == 128 ? launch_rows<128>(p, false, s) : launch_rows<256>(p, false, s);
+  return d == 64 ? launch_read<64>(p, s) : d == 96 ? launch_read<96>(p, s)
+       : d == 128 ? launch_read<128>(p, s) : launch_read<256>(p, s);
 }
 int launch_cache_attn(const CacheParams& p, int d, hipStream_t s) {
   return d == 64 ? launch_attn<64>(p, s) : d == 96 ? launch_attn<96>(p, s)
