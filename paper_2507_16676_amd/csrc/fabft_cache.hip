@@ -106,6 +106,13 @@ __device__ __forceinline__ bool nonfinite_bits(float x) {
   return (b & 0x7f800000u) == 0x7f800000u;
 }
 
+// A load; STREAM: of what nothing reads again soon, past the caches' other content.
+template <bool STREAM, class T>
+__device__ __forceinline__ T load_from(const void* a) {
+  const T* p = reinterpret_cast<const T*>(a);
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
 // by value: a conditional expression of two array elements would keep the array in memory
 __device__ __forceinline__ float pick(bool c, float a, float b) { return c ? a : b; }
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -400,21 +407,22 @@ struct KRegs {
   static constexpr int KW = D / 32;   // 32-bit words per lane and 16-key block
   uint32_t k[4][KW];
   uint32_t ks[D == 256 || D == 96 ? 2 : 1];
+  template <bool STREAM>
   __device__ __forceinline__ void load(const uint8_t* tile, const Lane<D>& ln) {
     constexpr CacheTile T(D);
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
       const uint8_t* a = tile + ln.koff + kb * 4 * T.row();
       if constexpr (KW == 2) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(a);
+        const u32x2 x = load_from<STREAM, u32x2>(a);
         k[kb][0] = x[0], k[kb][1] = x[1];
       } else if constexpr (KW == 3) {
-        const uint32_t* x = reinterpret_cast<const uint32_t*>(a);
-        k[kb][0] = x[0], k[kb][1] = x[1], k[kb][2] = x[2];
+#pragma unroll
+        for (int j = 0; j < 3; ++j) k[kb][j] = load_from<STREAM, uint32_t>(a + 4 * j);
       } else {
 #pragma unroll
         for (int j = 0; j < KW; j += 4) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(a + 4 * j);
+          const u32x4 x = load_from<STREAM, u32x4>(a + 4 * j);
           k[kb][j] = x[0], k[kb][j + 1] = x[1], k[kb][j + 2] = x[2], k[kb][j + 3] = x[3];
         }
       }
@@ -460,11 +468,12 @@ struct VRegs {
   u32x4 v[VC];
   uint32_t s[SW];
   u32x4 cs[2];
+  template <bool STREAM>
   __device__ __forceinline__ void load_codes(const uint8_t* tile, int lane) {
     constexpr CacheTile T(D);
 #pragma unroll
     for (int j = 0; j < VC; ++j)
-      v[j] = *reinterpret_cast<const u32x4*>(tile + T.vcode() + 1024 * j + 16 * lane);
+      v[j] = load_from<STREAM, u32x4>(tile + T.vcode() + 1024 * j + 16 * lane);
   }
   // key0: the first of the lane's keys
   __device__ __forceinline__ void load_scales(const uint8_t* tile, int key0, const Lane<D>& ln) {
@@ -653,7 +662,8 @@ __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& s
 // O^T = V^T P^T, as in the forward: a lane holds values of one query row (column
 // n = lane % 16), keys 16g .. 16g + 15 (g = lane / 16). The tiles go round the waves of all
 // splits, so that a wave's first tile depends on nothing that has to be loaded first.
-template <int D, int RP>
+// (STREAM: launch_attn.)
+template <int D, int RP, bool STREAM>
 __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void cache_attn_kernel(CacheParams p) {
   constexpr CacheTile T(D);
   using R = Rows<RP>;
@@ -692,8 +702,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
   VRegs<D, VPL> vr;
   {
     const uint8_t* tp = base + (size_t)min(t, p.tiles - 1) * T.bytes();
-    vr.load_codes(tp, lane);
-    kr.load(tp, ln);
+    vr.template load_codes<STREAM>(tp, lane);
+    kr.template load<STREAM>(tp, ln);
     vr.load_scales(tp, key0, ln);
   }
   u32x4 q[NT][KT];
@@ -743,7 +753,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
 #pragma unroll
     for (int j = 0; j < VRegs<D, VPL>::VC; ++j)
       *reinterpret_cast<u32x4*>(vl + v_chunk<D>(64 * j + lane)) = vr.v[j];
-    if constexpr (MORE) vr.load_codes(tp, lane);
+    if constexpr (MORE) vr.template load_codes<STREAM>(tp, lane);
     f32x4 s[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -758,7 +768,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
         for (int n = 0; n < NT; ++n) s[n][kb] = mfma16(a, q[n][kt], s[n][kb]);
       }
     }
-    if constexpr (MORE) kr.load(tp, ln);
+    if constexpr (MORE) kr.template load<STREAM>(tp, ln);
     float x[NT][VPL], mx[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) take_share<VPL>(s[n], ln.m, x[n]);
@@ -982,7 +992,7 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
   const int len_b = p.lengths[b], cnt_b = p.counts ? p.counts[b] : 0;
   int t = chunk * 4 + wave;
   KRegs<D> r;
-  r.load(base + (size_t)min(t, p.tiles - 1) * T.bytes(), ln);
+  r.template load<false>(base + (size_t)min(t, p.tiles - 1) * T.bytes(), ln);
   // rows c0 .. of q and their m, 1 / l: to LDS, by all
   auto stage = [&](int c0) __attribute__((always_inline)) {
     const int n = min(kWeightRows, p.R - c0);
@@ -1023,7 +1033,7 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) a[kb][kt] = r.operand(kb, kt, ln.g);
     const int tn = t + chunks * 4;
-    if (tn < tiles) r.load(base + (size_t)tn * T.bytes(), ln);
+    if (tn < tiles) r.template load<false>(base + (size_t)tn * T.bytes(), ln);
     // keys that some row that sees any does not see
     const bool edge = (t + 1) * kCacheTile > (p.causal ? seen.off + 1 : seen.len);
     float acc[16];
@@ -1115,17 +1125,28 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   if (g > INT_MAX || mg > INT_MAX) return -1;
   (void)hipGetLastError();
   const dim3 grid((unsigned)g), block(64 * kAttnWaves);
-  // One CU takes 60 GB/s or so from beyond its L2: 16 rows of 256 over 32 splits, 530 KB of
-  // records a row tile, took 14 us of 32 in the last workgroup, and 8 as a launch of its own; 33 KB
-  // (one row of 128, 64 splits) 5 and 7.
-  const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 200000;
+  // One CU takes 60 GB/s or so from beyond its L2: with 530 KB of records a row tile (16 rows of
+  // 256, 32 splits) the call took 32 us with the merge in the last workgroup and 23 with it as a
+  // launch of its own, with 135 KB (32 rows of 128, 8 splits) 66 and 60, with 67 KB (4 rows, 32
+  // splits) 16.9 and 17.2.
+  const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000;
   CacheParams p = p0;
   if (apart) p.tickets = nullptr;
-  if (rt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, 1>), grid, block, 0, s, p);
-  else if (rt == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 4>), grid, block, 0, s, p);
-  else if (rt == 8) hipLaunchKernelGGL((cache_attn_kernel<D, 8>), grid, block, 0, s, p);
-  else if (rt == 16) hipLaunchKernelGGL((cache_attn_kernel<D, 16>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((cache_attn_kernel<D, 32>), grid, block, 0, s, p);
+  // A cache that is read once per call and is large beside the 256 MB memory-side cache goes
+  // past it: 579 MB 108 us, 95 as a stream (6.0 TB/s), 114 MB 28.6 and 25.4. Below, what an
+  // earlier call left there counts for more (70 MB of three caches in turn 23.4 and 25.6).
+  const bool stream = p.n_rt == 1 && (long long)p.B * p.H * p.tiles * CacheTile(D).bytes() > (96 << 20);
+  auto launch = [&](auto RP) {
+    if (RP <= 16 && stream)
+      hipLaunchKernelGGL((cache_attn_kernel<D, RP, RP <= 16>), grid, block, 0, s, p);
+    else
+      hipLaunchKernelGGL((cache_attn_kernel<D, RP, false>), grid, block, 0, s, p);
+  };
+  if (rt == 1) launch(std::integral_constant<int, 1>{});
+  else if (rt == 4) launch(std::integral_constant<int, 4>{});
+  else if (rt == 8) launch(std::integral_constant<int, 8>{});
+  else if (rt == 16) launch(std::integral_constant<int, 16>{});
+  else launch(std::integral_constant<int, 32>{});
   if (apart) hipLaunchKernelGGL((cache_merge_kernel<D>), dim3((unsigned)mg), dim3(256), 0, s, p, rt);
   if (p.weight) {
     // about four workgroups per CU, each wave one tile or more
