@@ -106,6 +106,9 @@ __device__ __forceinline__ bool nonfinite_bits(float x) {
   return (b & 0x7f800000u) == 0x7f800000u;
 }
 
+// What is read or written once and is large beside the 256 MB memory-side cache goes past it.
+constexpr long long kStreamBytes = 96 << 20;
+
 // A load; STREAM: of what nothing reads again soon, past the caches' other content.
 template <bool STREAM, class T>
 __device__ __forceinline__ T load_from(const void* a) {
@@ -235,7 +238,7 @@ __device__ __forceinline__ void append_row(uint8_t* tile, int key, int lane, boo
 // 2 and 4 bytes; lines that several XCDs write in parts cost more) and has more on its way.
 // (4 x 32 heads, 4,096 rows of 128: 80 us with 16 rows a workgroup and a division for s and
 // 1 / s each, 65 now: 5.3 TB/s, the rate of a large copy.)
-template <int D, int ITER>
+template <int D, int ITER, bool STREAM>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
   constexpr int N = RowLanes<D>::N, ROWS = RowLanes<D>::ROWS;
   constexpr CacheTile T(D);
@@ -263,8 +266,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
     const int i = i0 + it * ROWS;
     k[it] = v[it] = u32x4{0, 0, 0, 0};
     if (live && i < n) {
-      k[it] = *reinterpret_cast<const u32x4*>(p.k + b * p.kb + h * p.kh + i * p.kn + 8 * lane);
-      v[it] = *reinterpret_cast<const u32x4*>(p.v + b * p.vb + h * p.vh + i * p.vn + 8 * lane);
+      k[it] = load_from<STREAM, u32x4>(p.k + b * p.kb + h * p.kh + i * p.kn + 8 * lane);
+      v[it] = load_from<STREAM, u32x4>(p.v + b * p.vb + h * p.vh + i * p.vn + 8 * lane);
     }
   }
 #pragma unroll
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRows p) {
 }
 
 // ---- read: the values of a row, zeros for rows that are not in the cache
-template <int D>
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRows p) {
   constexpr int N = RowLanes<D>::N;
   constexpr CacheTile T(D);
@@ -304,8 +307,15 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRows p) {
     for (int j = 0; j < 4; ++j)   // exact: 6 bits times 2
       v[j] = pack_bf16x2(__uint_as_float(x[j] << 16) * sf, __uint_as_float(x[j] & 0xffff0000u) * sf);
   }
-  *reinterpret_cast<u32x4*>(p.k + row * D + 8 * lane) = k;
-  *reinterpret_cast<u32x4*>(p.v + row * D + 8 * lane) = v;
+  u32x4* kp = reinterpret_cast<u32x4*>(p.k + row * D + 8 * lane);
+  u32x4* vp = reinterpret_cast<u32x4*>(p.v + row * D + 8 * lane);
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store(k, kp);
+    __builtin_nontemporal_store(v, vp);
+  } else {
+    *kp = k;
+    *vp = v;
+  }
 }
 
 // ---- attention
@@ -1132,10 +1142,11 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000;
   CacheParams p = p0;
   if (apart) p.tickets = nullptr;
-  // A cache that is read once per call and is large beside the 256 MB memory-side cache goes
-  // past it: 579 MB 108 us, 95 as a stream (6.0 TB/s), 114 MB 28.6 and 25.4. Below, what an
-  // earlier call left there counts for more (70 MB of three caches in turn 23.4 and 25.6).
-  const bool stream = p.n_rt == 1 && (long long)p.B * p.H * p.tiles * CacheTile(D).bytes() > (96 << 20);
+  // A stream where every tile is read once: 579 MB 108 us, 93 as a stream (6.1 TB/s), 114 MB 28.6
+  // and 26.4. Where what an earlier call left in the memory-side cache is read again, it costs
+  // (three caches in turn, 70 MB each: 23.4 and 25.3).
+  const bool stream =
+      p.n_rt == 1 && (long long)p.B * p.H * p.tiles * CacheTile(D).bytes() > kStreamBytes;
   auto launch = [&](auto RP) {
     if (RP <= 16 && stream)
       hipLaunchKernelGGL((cache_attn_kernel<D, RP, RP <= 16>), grid, block, 0, s, p);
@@ -1443,8 +1454,13 @@ int launch_append(const CacheRows& p, hipStream_t s) {
   const long long g = many ? heads * ((p.n + 63) / 64) : (heads * p.n + ROWS - 1) / ROWS;
   if (g > INT_MAX) return -1;
   (void)hipGetLastError();
-  if (many) hipLaunchKernelGGL((cache_append_kernel<D, ITER>), dim3((unsigned)g), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((cache_append_kernel<D, 1>), dim3((unsigned)g), dim3(256), 0, s, p);
+  const dim3 grid((unsigned)g), block(256);
+  if (many && heads * p.n * 4 * D > kStreamBytes)
+    hipLaunchKernelGGL((cache_append_kernel<D, ITER, true>), grid, block, 0, s, p);
+  else if (many)
+    hipLaunchKernelGGL((cache_append_kernel<D, ITER, false>), grid, block, 0, s, p);
+  else
+    hipLaunchKernelGGL((cache_append_kernel<D, 1, false>), grid, block, 0, s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -1454,7 +1470,10 @@ int launch_read(const CacheRows& p, hipStream_t s) {
   const long long g = (rows + RowLanes<D>::ROWS - 1) / RowLanes<D>::ROWS;
   if (g > INT_MAX) return -1;
   (void)hipGetLastError();
-  hipLaunchKernelGGL((cache_read_kernel<D>), dim3((unsigned)g), dim3(256), 0, s, p);
+  const dim3 grid((unsigned)g), block(256);
+  // (4 x 32 heads x 4,096 rows of 128, 268 MB of values: 58 -> 49 us)
+  if (rows * 4 * D > kStreamBytes) hipLaunchKernelGGL((cache_read_kernel<D, true>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((cache_read_kernel<D, false>), grid, block, 0, s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
