@@ -62,6 +62,7 @@ struct CacheParams {
   int tiles;            // capacity in tiles
   int Lq, R;            // query rows per query head, per key/value head
   int causal, nsplit, n_rt;
+  int by_length;        // workgroups take the longest sequences first
   int wcheck;
   float sl2, decay, tau_rel, tau_abs;
 };

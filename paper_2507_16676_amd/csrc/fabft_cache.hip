@@ -564,6 +564,18 @@ __device__ __forceinline__ int used_splits(int tiles, int nsplit) {
   return tiles <= kCacheFewTiles ? 1 : min(nsplit, (tiles + kAttnWaves - 1) / kAttnWaves);
 }
 
+// The sequence that has n longer ones (of equal ones the first comes first), of up to 64; by a
+// whole wave.
+__device__ __forceinline__ int nth_longest(const CacheParams& p, int n, int lane) {
+  const int len = lane < p.B ? clampi(p.lengths[lane], 0, p.tiles * kCacheTile) : -1;
+  int rank = 0;
+  for (int i = 0; i < p.B; ++i) {
+    const int x = __builtin_amdgcn_readlane(len, i);
+    rank += x > len || (x == len && i < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < p.B && rank == n));
+}
+
 __device__ __forceinline__ void put(float* a, float x) {
   __hip_atomic_store(a, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -698,7 +710,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
     in = j % inner;
   }
   const int rt = in / p.nsplit, split = in - rt * p.nsplit;
-  const int b = bh / p.H, r0 = rt * RP;
+  const int r0 = rt * RP;
+  int b = bh / p.H;
+  if (p.by_length) {   // the b-th longest sequence
+    b = nth_longest(p, b, lane);
+    bh = b * p.H + bh % p.H;
+  }
   const Lane<D> ln(lane, p.wcheck != 0);
   const int key0 = 16 * ln.g + (RP < 16 ? ln.m / RP * VPL : 0);   // the first of the lane's keys
   const size_t row0 = (size_t)bh * p.R;
@@ -1141,6 +1158,9 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   // splits) 16.9 and 17.2.
   const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000;
   CacheParams p = p0;
+  // More workgroups than fit at once: the longest sequences first, so that none of them starts
+  // when the others end.
+  p.by_length = p.n_rt > 1 && p.B > 1 && p.B <= 64 && g > 512;
   if (apart) p.tickets = nullptr;
   // A stream where every tile is read once: 579 MB 108 us, 93 as a stream (6.1 TB/s), 114 MB 28.6
   // and 26.4. Where what an earlier call left in the memory-side cache is read again, it costs
