@@ -1253,7 +1253,28 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
   __shared__ int sh_bin, sh_above;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bh = blockIdx.x, b = bh / p.H;
-  const int len = clampi(__builtin_amdgcn_readfirstlane(p.lengths[b]), 0, p.tiles * kCacheTile);
+  const int slots = p.tiles * kCacheTile;
+  const float* w = p.weight + (size_t)bh * slots;
+  uint32_t u[K];
+  auto load = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = c0 + k * THREADS;
+      u[k] = 0;
+      if (i + THREADS <= slots) u[k] = __float_as_uint((w + i)[tid]);   // (the same for all)
+      else if (i + tid < slots) u[k] = __float_as_uint((w + i)[tid]);
+    }
+  };
+  auto order = [&](int c0, int old) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (c0 + k * THREADS < old) u[k] = order_of(__uint_as_float(u[k]));
+    }
+  };
+  const int len_b = p.lengths[b];
+  load(0);   // before the length is known: every slot has a weight
+  for (int j = tid; j < 3 * skew(2048); j += THREADS) hists[0][j] = 0;
+  const int len = clampi(__builtin_amdgcn_readfirstlane(len_b), 0, slots);
   const int kept = min(len, p.keep);
   int* index = p.index + (size_t)bh * p.keep;
   if (tid == 0 && bh == b * p.H) p.new_lengths[b] = kept;
@@ -1262,27 +1283,11 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
     for (int j = tid; j < len; j += THREADS) index[j] = j;
     return;
   }
-  const float* w = p.weight + (size_t)bh * p.tiles * kCacheTile;
   const int old = len - min(p.recent, p.keep);   // candidates: slots [0, old)
   const int want = kept - (len - old);           // of them to keep, < old
   for (int j = tid; j < len - old; j += THREADS) index[want + j] = old + j;
   if (want <= 0) return;
-  for (int j = tid; j < 3 * skew(2048); j += THREADS) hists[0][j] = 0;
-  uint32_t u[K];
-  auto load = [&](int c0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int i = c0 + k * THREADS;
-      u[k] = 0;
-      if (i + THREADS <= old) u[k] = __float_as_uint((w + i)[tid]);   // (the same for all)
-      else if (i + tid < old) u[k] = __float_as_uint((w + i)[tid]);
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (c0 + k * THREADS < old) u[k] = order_of(__uint_as_float(u[k]));
-    }
-  };
-  load(0);
+  order(0, old);
   uint32_t prefix = 0;
   int need = want;   // how many of the candidates with the prefix to keep
 #pragma unroll
@@ -1291,7 +1296,10 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
     int* hist = hists[pass];
     if (pass == 0) __syncthreads();
     for (int c0 = 0; c0 < old; c0 += CHUNK) {
-      if (old > CHUNK) load(c0);
+      if (old > CHUNK) {
+        load(c0);
+        order(c0, old);
+      }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int i = c0 + k * THREADS;
@@ -1313,7 +1321,10 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(CacheEvict p) {
   const uint64_t below = (1ull << lane) - 1;
   int ng0 = 0, ne0 = 0;   // of the chunks before
   for (int c0 = 0; c0 < old; c0 += CHUNK) {
-    if (old > CHUNK) load(c0);
+    if (old > CHUNK) {
+      load(c0);
+      order(c0, old);
+    }
     __syncthreads();
     for (int j = tid; j < skew(K * W); j += THREADS) cnt[0][j] = cnt[1][j] = 0;
     __syncthreads();
@@ -1380,32 +1391,32 @@ __global__ __launch_bounds__(kEvictThreads) void cache_move_kernel(CacheEvict p,
   const int part = blockIdx.x & 1;
   const int chunk = (blockIdx.x >> 1) % batches;
   const int bh = (blockIdx.x >> 1) / batches;
-  const int len = clampi(p.lengths[bh / p.H], 0, p.tiles * kCacheTile);
-  const int kept = min(len, p.keep);
-  const int* index = p.index + (size_t)bh * p.keep;
+  const int len_b = p.lengths[bh / p.H];
+  const int* index = p.index + (size_t)bh * p.keep;   // -1 behind the kept ones
   const uint8_t* src = p.cache + (size_t)bh * p.tiles * T.bytes();
   uint8_t* dst = p.into + (size_t)bh * p.into_tiles * T.bytes();
   const float* w = p.weight + (size_t)bh * p.tiles * kCacheTile;
   float* nw = p.into_weight + (size_t)bh * p.into_tiles * kCacheTile;
   const int codes = part ? T.vcode() : 0;
-  for (int j0 = chunk * BATCH; j0 < kept; j0 += batches * BATCH) {
+  for (int j0 = chunk * BATCH; j0 < p.keep; j0 += batches * BATCH) {
     u32x4 c[NC];
+    int from[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) from[k] = index[min(j0 + (k * kEvictThreads + tid) / CH, p.keep - 1)];
+    // the small parts: one row per thread
+    const int j = j0 + tid, i = index[min(j, p.keep - 1)];
+    const bool mine = j < p.keep && i >= 0;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int e = k * kEvictThreads + tid, j = j0 + e / CH;
-      if (j < kept) {
-        const int i = index[j];
-        c[k] = *reinterpret_cast<const u32x4*>(src + (size_t)(i / kCacheTile) * T.bytes() + codes +
-                                               (i % kCacheTile) * T.row() + 16 * (e % CH));
-      }
+      const int e = k * kEvictThreads + tid, f = from[k];
+      if (f >= 0)
+        c[k] = *reinterpret_cast<const u32x4*>(src + (size_t)(f / kCacheTile) * T.bytes() + codes +
+                                               (f % kCacheTile) * T.row() + 16 * (e % CH));
     }
-    // the small parts: one row per thread
-    const int j = j0 + tid;
     uint8_t ks[T.blocks()];
     uint16_t vs[5];
     float wt = 0.f;
-    if (j < kept) {
-      const int i = index[j];
+    if (mine) {
       const uint8_t* tile = src + (size_t)(i / kCacheTile) * T.bytes();
       if (part == 0) {
 #pragma unroll
@@ -1424,11 +1435,11 @@ __global__ __launch_bounds__(kEvictThreads) void cache_move_kernel(CacheEvict p,
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
       const int e = k * kEvictThreads + tid, jj = j0 + e / CH;
-      if (jj < kept)
+      if (jj < p.keep && from[k] >= 0)
         *reinterpret_cast<u32x4*>(dst + (size_t)(jj / kCacheTile) * T.bytes() + codes +
                                   (jj % kCacheTile) * T.row() + 16 * (e % CH)) = c[k];
     }
-    if (j < kept) {
+    if (mine) {
       uint8_t* tile = dst + (size_t)(j / kCacheTile) * T.bytes();
       if (part == 0) {
 #pragma unroll
@@ -1442,6 +1453,7 @@ __global__ __launch_bounds__(kEvictThreads) void cache_move_kernel(CacheEvict p,
       }
     }
   }
+  const int kept = min(clampi(len_b, 0, p.tiles * kCacheTile), p.keep);
   // the slots behind them have no weight. In place the same workgroup has read all it
   // needs of them by now
   if (part == 0)
