@@ -524,7 +524,7 @@ def global_check(o, resid):
 CACHE_TILE = 64
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class Cache:
     """A key/value cache held in 4 bits (fabft_cache_bytes in include/fabft.h): `data` is the
     buffer, its layout the library's; `capacity` the slots per head, a multiple of CACHE_TILE.

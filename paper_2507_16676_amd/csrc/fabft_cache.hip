@@ -1041,9 +1041,7 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
     if (ln.m >= p.R) st1[1] = 0.f;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
-      // (rows that add nothing: their q may hold anything)
-      q1[kt] = st1[1] > 0.f ? *reinterpret_cast<const u32x4*>(p.q + row * D + ln.g * (D / 4) + 8 * kt)
-                            : u32x4{0, 0, 0, 0};
+      q1[kt] = *reinterpret_cast<const u32x4*>(p.q + row * D + ln.g * (D / 4) + 8 * kt);
   }
   const Seen seen(p, len_b, cnt_b);
   const int tiles = (seen.len + kCacheTile - 1) / kCacheTile;
@@ -1066,7 +1064,9 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
     float acc[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-    auto rows16 = [&](const u32x4 (&q)[KT], const f32x4& st) __attribute__((always_inline)) {
+    // rows that add nothing (1 / l = 0) have to, whatever their q and the keys hold, NaN too:
+    // one operand by a product that is 0 then, several by the mask (st[2] is -1)
+    auto rows16 = [&](const u32x4 (&q)[KT], const f32x4& st, bool mask) __attribute__((always_inline)) {
       f32x4 s[4];
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) s[kb] = f32x4{0, 0, 0, 0};
@@ -1074,19 +1074,21 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) s[kb] = mfma16(a[kb][kt], q[kt], s[kb]);
-      if (edge) {
+      if (mask) {
         asm volatile("");   // (a branch)
         const int lim = __float_as_int(st[2]) - t * kCacheTile - 16 * ln.g;
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j / 4][j & 3] = j <= lim ? s[j / 4][j & 3] : -kInf;
       }
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        acc[j] = __builtin_fmaf(
-            __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j & 3], p.sl2, -st[0])), st[1], acc[j]);
+      for (int j = 0; j < 16; ++j) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j & 3], p.sl2, -st[0]));
+        if constexpr (MANY) acc[j] = __builtin_fmaf(e, st[1], acc[j]);
+        else acc[j] = mul_zero(e, st[1]);
+      }
     };
     if constexpr (!MANY) {
-      rows16(q1, st1);
+      rows16(q1, st1, edge);
     } else {
       for (int c0 = 0; c0 < p.R; c0 += kWeightRows) {
         if (p.R > kWeightRows) {
@@ -1099,19 +1101,12 @@ __global__ __launch_bounds__(256, 2) void cache_weight_kernel(CacheParams p, int
         for (int r0 = 0; r0 < n; r0 += 16) {
           const int i = min(r0 + ln.m, n - 1);
           f32x4 st = lst[i];
-          if (r0 + ln.m >= n) st[1] = 0.f;
+          if (r0 + ln.m >= n) st = f32x4{kInf, 0.f, __int_as_float(-1), 0.f};
           u32x4 q[KT];
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt)
             q[kt] = *reinterpret_cast<const u32x4*>(lq + i * QS + ln.g * (D / 2) + 16 * kt);
-          if (__any(!(st[1] > 0.f))) {
-            asm volatile("");   // (a branch) rows that add nothing: their q may hold anything
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) q[kt][e] = st[1] > 0.f ? q[kt][e] : 0;
-          }
-          rows16(q, st);
+          rows16(q, st, edge || __any(!(st[1] > 0.f)));
         }
       }
       if (!work) continue;

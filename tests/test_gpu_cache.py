@@ -212,6 +212,98 @@ def test_attention(case):
     check_attention(q, c, ke, ve, lens, cnt, causal, 0.0, weight=weight, decay=0.0, nsplit=ns)
 
 
+# more than 12 tiles: the splits are merged, in the last workgroup, or with many rows and splits
+# by a launch of their own; 1, up to 4, 8, 16 and 32 rows a workgroup, and several of those
+MERGES = [
+    # B, H, G, Lq, capacity, d, lengths, nsplit
+    (2, 2, 1, 1, 2048, 128, [2047, 833], None),
+    (4, 1, 1, 1, 3200, 64, [3200, 70, 0, 1500], 13),
+    (1, 3, 3, 1, 1600, 96, [1599], 5),
+    (2, 8, 2, 2, 1024, 256, [1024, 900], 4),
+    (1, 2, 8, 1, 6400, 128, [6399], 64),          # apart
+    (3, 1, 2, 4, 1500, 64, [1500, 2, 1100], 7),
+    (1, 1, 4, 4, 5000, 256, [4999], 32),          # apart
+    (2, 2, 5, 2, 1700, 96, [1700, 1300], 9),
+    (1, 1, 2, 16, 2100, 128, [2050], 3),
+    (1, 2, 1, 29, 2304, 64, [2304], 31),          # apart
+    (2, 1, 3, 37, 1100, 128, [1100, 850], 4),     # several row tiles
+    (1, 1, 1, 70, 1300, 256, [1290], 5),
+]
+
+
+@pytest.mark.parametrize("case", MERGES, ids=lambda c: "b{}h{}g{}q{}c{}d{}".format(*c[:6]))
+def test_merge(case):
+    B, H, Gq, Lq, cap, d, lengths, ns = case
+    print(f"[cache merge] {case}", flush=True)
+    c, ke, ve = filled(B, H, -(-cap // 64) * 64, d, 35)
+    q = draw(36, B, H * Gq, Lq, d)
+    weight = torch.rand((B, H, c.capacity), device="cuda")
+    w0 = weight.clone()
+    a = check_attention(q, c, ke, ve, lengths, None, True, d ** -0.5, weight=weight, nsplit=ns)
+    for _ in range(5):     # whichever workgroup comes last: bit for bit
+        w = w0.clone()
+        b = F.attn_fwd_cache(q, c, ints(lengths), causal=True, nsplit=ns, weight=w)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(w, weight)
+    # and as without splits, to rounding
+    one, _, _ = F.attn_fwd_cache(q, c, ints(lengths), causal=True, nsplit=1)
+    assert float((one.float() - a[0].float()).abs().max()) <= 2.0 ** -6 * float(one.float().abs().max())
+
+
+def test_longest_first():
+    """More workgroups than fit at once, of sequences of different lengths and row counts."""
+    B, H, Gq, Lq, cap, d = 4, 16, 2, 192, 448, 64
+    c, ke, ve = filled(B, H, cap, d, 37)
+    check_attention(draw(38, B, H * Gq, Lq, d), c, ke, ve, [200, 448, 0, 448], [192, 100, 7, 192], True,
+                    d ** -0.5, weight=torch.zeros((B, H, cap), device="cuda"))
+
+
+def test_large_caches():
+    """Caches beside which the memory-side cache is small are read, filled and listed as streams:
+    the results are those of a small one, bit for bit."""
+    H, d, n = 8, 128, 1100
+    c, ke, ve = filled(1, H, 1152, d, 39)
+    big = F.cache_new(1, H, 131072, d)
+    k, v = F.cache_read(c, ints([0]), n)
+    F.cache_append(big, k, v, ints([0]))      # (the values are their own nearest ones)
+    for G, Lq in ((1, 1), (4, 1), (8, 1), (4, 4)):
+        q = draw(40, 1, H * G, Lq, d)
+        for ns in (1, 4):
+            a = F.attn_fwd_cache(q, c, ints([n]), causal=True, nsplit=ns)
+            b = F.attn_fwd_cache(q, big, ints([n]), causal=True, nsplit=ns)
+            assert torch.equal(a[0], b[0]) and int(b[2].sum()) == 0
+    n, d = 98_500, 256
+    k, v = draw(41, 1, 1, n, d), draw(42, 1, 1, n, d)
+    c = F.cache_new(1, 1, n, d)
+    F.cache_append(c, k, v, ints([0]))
+    kr, vr = F.cache_read(c, ints([0]), n)
+    for at in (0, 40_000, n - 3000):
+        part = F.cache_new(1, 1, 3008, d)
+        F.cache_append(part, k[:, :, at:at + 3000], v[:, :, at:at + 3000], ints([0]))
+        kp, vp = F.cache_read(part, ints([0]), 3000)
+        assert torch.equal(kr[:, :, at:at + 3000], kp) and torch.equal(vr[:, :, at:at + 3000], vp)
+
+
+@pytest.mark.parametrize("rows", [(1, 3), (4, 17)])
+def test_nan_keys_leave_the_weights(rows):
+    """Keys of NaN in the middle of the cache: all rows that see them are flagged and add nothing,
+    the keys' own weights included; rows that do not see them add theirs."""
+    G, Lq = rows
+    H, cap, d = 2, 320, 64
+    k, v = draw(43, 1, H, cap, d), draw(44, 1, H, cap, d)
+    k[0, 0, 100, 5] = float("nan")
+    v[0, 1, 305, 7] = float("inf")
+    c = F.cache_new(1, H, cap, d)
+    F.cache_append(c, k, v, ints([0]))
+    w = torch.full((1, H, cap), 0.5, device="cuda")
+    q = draw(45, 1, H * G, Lq, d)
+    o, _, flags = F.attn_fwd_cache(q, c, ints([cap]), causal=True, weight=w)
+    assert bool((flags[:, :G] & F.FLAG_NONFINITE).bool().all()) and bool((w[:, 0] == 0.5).all())
+    seen = torch.arange(cap - Lq, cap, device="cuda") >= 305
+    assert torch.equal((flags[0, G:] != 0), seen.expand(G, Lq))
+    assert bool(torch.isfinite(w).all())
+    assert abs(float(w[0, 1].double().sum()) - 0.5 * cap - G * int((~seen).sum())) < 1e-3
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_attention_peaked(d):
     """Scores that jump late past the lazily kept maximum, and far below it."""
@@ -465,14 +557,16 @@ def test_decode_with_eviction(d):
     decode_loop(60, 2, 2, 2, d, 64, 48, 16, one_step)
 
 
-def test_decode_from_a_graph():
+@pytest.mark.parametrize("cap,Gq,n", [(640, 2, 500), (4096, 2, 3000), (4160, 12, 4100)])
+def test_decode_from_a_graph(cap, Gq, n):
     """The step captured once on another stream, replayed with new tokens and lengths between eager
-    work; every replay against an eager twin, bit for bit."""
-    B, H, Gq, d, cap = 2, 2, 2, 128, 640
+    work (one workgroup a head, the merge of splits in the last one, and apart); every replay
+    against an eager twin, bit for bit."""
+    B, H, d = 2, 2, 128
     caches = [filled(B, H, cap, d, 53)[0] for _ in range(2)]
     ws = [torch.zeros((B, H, cap), device="cuda") for _ in range(2)]
     q, k, v = draw(60, B, H * Gq, 1, d), draw(61, B, H, 1, d), draw(62, B, H, 1, d)
-    lengths = ints([500, 63])
+    lengths = ints([n, 63])
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
