@@ -467,7 +467,11 @@ int fabft_attn_fwd_debug(const void* q, const void* k, const void* v,
  * slots (keys) per head. The library keeps no lengths: every call is told them
  * in device arrays of B ints, so that it can be captured into a graph whose
  * replays see their current values. A slot that was never written may hold
- * anything. All four calls are asynchronous on the library stream.
+ * anything. All four calls are asynchronous on the library stream. More than a
+ * launch holds (2^32 threads; FABFT_E_SHAPE, and nothing ran) is 2^24 workgroups:
+ * of append 64 rows of a head (n < 64: 2048 / d rows), of the attention a split of
+ * 1, 4, 8, 16 or 32 query rows; 2^21 heads, or more and 1024 slots of a head each,
+ * of evict.
  */
 long long fabft_cache_bytes(int B, int H, int capacity, int d);
 
@@ -475,7 +479,7 @@ long long fabft_cache_bytes(int B, int H, int capacity, int d);
  * Row i < n of k and v (bf16, [B, H, n, d]) of sequence b goes to slot
  * start[b] + i. counts (may be NULL: all n): only rows i < counts[b]. A row
  * whose slot is not in [0, capacity) is dropped; slots that no row goes to
- * stay as they were. strides: NULL for contiguous k and v, else a HOST array
+ * stay as they were. n: at most 2^30. strides: NULL for contiguous k and v, else a HOST array
  * of the strides, in elements, of k over b, h and i, and of v over b, h and i:
  * multiples of 8 (FABFT_E_ALIGN); the channels are contiguous.
  */
@@ -486,7 +490,7 @@ int fabft_cache_append(void* cache, int B, int H, int capacity, int d,
 
 /*
  * The values of slots start[b] + i, i < n, into k and v (bf16, [B, H, n, d],
- * contiguous); zeros for rows i >= counts[b] and for slots not in
+ * contiguous; n at most 2^30); zeros for rows i >= counts[b] and for slots not in
  * [0, capacity).
  */
 int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
@@ -514,8 +518,8 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * nsplit: 1..64 ranges of whole 64-key tiles per row, merged by the last
  * workgroup of a row to finish; fabft_cache_splits gives the library's choice. A workspace
  * (16-byte aligned, overwritten) of fabft_cache_workspace_bytes bytes is needed
- * where that is not 0 (nsplit > 1, or with weight). H * G, B * H * G * Lq and
- * the grid must fit 31 bits (FABFT_E_SHAPE).
+ * where that is not 0 (nsplit > 1, or with weight). B * H * G * Lq is at most 2^30
+ * (FABFT_E_SHAPE). q and o must not overlap.
  */
 int fabft_attn_fwd_cache(const void* q, const void* cache, void* o,
                          float* resid, uint8_t* flags, int B, int H, int G,

@@ -567,6 +567,10 @@ unsigned long long next_nonce() {
   return x;
 }
 
+int launched(int rc) {
+  return rc == 0 ? FABFT_OK : rc == fabft::kCacheGrid ? FABFT_E_SHAPE : FABFT_E_LAUNCH;
+}
+
 bool splits_ok(int nsplit) { return nsplit >= 1 && nsplit <= kMaxSplits; }
 
 }  // namespace
@@ -585,7 +589,7 @@ int fabft_cache_append(void* cache, int B, int H, int capacity, int d, const voi
   if (!k || !v || !start) return FABFT_E_NULL;
   int rc = cache_ok(cache, B, H, capacity, d);
   if (rc != FABFT_OK) return rc;
-  if (n < 1 || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
+  if (n < 1 || n > fabft::kCacheMostRows || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
   if (!aligned16(k) || !aligned16(v)) return FABFT_E_ALIGN;
   const long long nd = static_cast<long long>(n) * d;
   const long long dense[6] = {H * nd, nd, d, H * nd, nd, d};
@@ -601,8 +605,7 @@ int fabft_cache_append(void* cache, int B, int H, int capacity, int d, const voi
   p.start = start;
   p.counts = counts;
   p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile, p.n = n;
-  rc = fabft::launch_cache_append(p, d, g_stream);
-  return rc == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+  return launched(fabft::launch_cache_append(p, d, g_stream));
 }
 
 int fabft_cache_read(const void* cache, int B, int H, int capacity, int d, void* k, void* v, int n,
@@ -610,7 +613,7 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d, void*
   if (!k || !v || !start) return FABFT_E_NULL;
   int rc = cache_ok(cache, B, H, capacity, d);
   if (rc != FABFT_OK) return rc;
-  if (n < 1 || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
+  if (n < 1 || n > fabft::kCacheMostRows || cache_size(B, H, capacity, d) < 0) return FABFT_E_SHAPE;
   if (!aligned16(k) || !aligned16(v)) return FABFT_E_ALIGN;
   fabft::CacheRows p{};
   p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
@@ -619,13 +622,12 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d, void*
   p.start = start;
   p.counts = counts;
   p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile, p.n = n;
-  rc = fabft::launch_cache_read(p, d, g_stream);
-  return rc == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+  return launched(fabft::launch_cache_read(p, d, g_stream));
 }
 
 int fabft_cache_splits(int B, int H, int G, int Lq, int capacity) {
   if (B < 1 || H < 1 || G < 1 || Lq < 1 || capacity < 1 || capacity > (1 << 30) ||
-      static_cast<long long>(G) * Lq > INT_MAX)
+      static_cast<__int128>(B) * H * G * Lq > fabft::kCacheMostRows)
     return FABFT_E_SHAPE;
   return fabft::cache_splits(B, H, G * Lq, (capacity + fabft::kCacheTile - 1) / fabft::kCacheTile);
 }
@@ -635,7 +637,7 @@ long long fabft_cache_workspace_bytes(int B, int H, int G, int Lq, int d, int ns
   if (!head_dim_ok(d)) return FABFT_E_HEADDIM;
   if (B < 1 || H < 1 || G < 1 || Lq < 1 || !splits_ok(nsplit)) return FABFT_E_SHAPE;
   const __int128 rows = static_cast<__int128>(B) * H * G * Lq;
-  if (rows > INT_MAX) return FABFT_E_SHAPE;
+  if (rows > fabft::kCacheMostRows) return FABFT_E_SHAPE;
   const long long n = static_cast<long long>(rows);
   // the rows' m and l; records and tickets of the splits
   const int rt = fabft::cache_row_tile(G * Lq);
@@ -687,9 +689,7 @@ int fabft_attn_fwd_cache(const void* q, const void* cache, void* o, float* resid
   p.decay = decay;
   p.tau_rel = g_tau_rel;
   p.tau_abs = g_tau_abs;
-  // the grid
-  if (static_cast<long long>(B) * H * p.n_rt * nsplit > INT_MAX) return FABFT_E_SHAPE;
-  return fabft::launch_cache_attn(p, d, g_stream) == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+  return launched(fabft::launch_cache_attn(p, d, g_stream));
 }
 
 int fabft_cache_evict(void* cache, int B, int H, int capacity, int d, float* weight,
@@ -722,7 +722,7 @@ int fabft_cache_evict(void* cache, int B, int H, int capacity, int d, float* wei
   p.B = B, p.H = H, p.tiles = capacity / fabft::kCacheTile;
   p.into_tiles = into_capacity / fabft::kCacheTile;
   p.keep = keep, p.recent = recent;
-  return fabft::launch_cache_evict(p, d, g_stream) == 0 ? FABFT_OK : FABFT_E_LAUNCH;
+  return launched(fabft::launch_cache_evict(p, d, g_stream));
 }
 
 }  // extern "C"

@@ -106,6 +106,12 @@ inline int cache_splits(int B, int H, int R, int tiles) {
 }
 inline int cache_record_floats(int d) { return d + 4; }
 
+// 0, -1 (the launch failed) or kCacheGrid: the call is more than a grid holds, and nothing ran.
+constexpr int kCacheGrid = -2;
+// Rows n of an append or a read, and query rows B * H * G * Lq: then no 32-bit index of a row,
+// or of the first row of a tile behind the last, overflows.
+constexpr int kCacheMostRows = 1 << 30;
+
 int launch_cache_append(const CacheRows& p, int d, hipStream_t s);
 int launch_cache_read(const CacheRows& p, int d, hipStream_t s);
 int launch_cache_attn(const CacheParams& p, int d, hipStream_t s);

@@ -109,6 +109,9 @@ __device__ __forceinline__ bool nonfinite_bits(float x) {
 // What is read or written once and is large beside the 256 MB memory-side cache goes past it.
 constexpr long long kStreamBytes = 96 << 20;
 
+// A launch has at most 2^32 - 1 threads along a dimension of its grid.
+bool grid_ok(long long groups, int threads) { return groups <= (long long)(UINT32_MAX / threads); }
+
 // A load; STREAM: of what nothing reads again soon, past the caches' other content.
 template <bool STREAM, class T>
 __device__ __forceinline__ T load_from(const void* a) {
@@ -286,7 +289,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRows p) {
   constexpr int N = RowLanes<D>::N;
   constexpr CacheTile T(D);
   const int lane = threadIdx.x % N;
-  const long long row = (long long)blockIdx.x * RowLanes<D>::ROWS + threadIdx.x / N;
+  const long long row =
+      ((long long)blockIdx.y * gridDim.x + blockIdx.x) * RowLanes<D>::ROWS + threadIdx.x / N;
   const long long bh = row / p.n;
   const int i = (int)(row - bh * p.n);
   if (bh >= (long long)p.B * p.H || lane >= D / 8) return;
@@ -1143,8 +1147,11 @@ template <int D>
 int launch_attn(const CacheParams& p0, hipStream_t s) {
   const int rt = cache_row_tile(p0.R);
   const long long g = (long long)p0.B * p0.H * p0.n_rt * p0.nsplit;
-  const long long mg = (long long)p0.B * p0.H * ((p0.R + 3) / 4);
-  if (g > INT_MAX || mg > INT_MAX) return -1;
+  const long long heads = (long long)p0.B * p0.H, mg = heads * ((p0.R + 3) / 4);
+  // the weights: about four workgroups per CU, each wave one tile or more
+  const int most = (p0.tiles + 3) / 4;
+  long long ch = (1024 + heads - 1) / heads;
+  if (ch > most) ch = most;
   (void)hipGetLastError();
   const dim3 grid((unsigned)g), block(64 * kAttnWaves);
   // One CU takes 60 GB/s or so from beyond its L2: with 530 KB of records a row tile (16 rows of
@@ -1152,6 +1159,8 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   // launch of its own, with 135 KB (32 rows of 128, 8 splits) 66 and 60, with 67 KB (4 rows, 32
   // splits) 16.9 and 17.2.
   const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000;
+  if (!grid_ok(g, 64 * kAttnWaves) || (apart && !grid_ok(mg, 256)) || (p0.weight && !grid_ok(heads * ch, 256)))
+    return kCacheGrid;
   CacheParams p = p0;
   // More workgroups than fit at once: the longest sequences first, so that none of them starts
   // when the others end.
@@ -1175,12 +1184,6 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   else launch(std::integral_constant<int, 32>{});
   if (apart) hipLaunchKernelGGL((cache_merge_kernel<D>), dim3((unsigned)mg), dim3(256), 0, s, p, rt);
   if (p.weight) {
-    // about four workgroups per CU, each wave one tile or more
-    const long long heads = (long long)p.B * p.H;
-    const int most = (p.tiles + 3) / 4;
-    long long ch = (1024 + heads - 1) / heads;
-    if (ch > most) ch = most;
-    if (heads * ch > INT_MAX) return -1;
     const dim3 wg((unsigned)(heads * ch));
     if (p.R > 16) hipLaunchKernelGGL((cache_weight_kernel<D, true>), wg, dim3(256), 0, s, p, (int)ch);
     else hipLaunchKernelGGL((cache_weight_kernel<D, false>), wg, dim3(256), 0, s, p, (int)ch);
@@ -1461,7 +1464,7 @@ template <int D>
 int launch_evict(const CacheEvict& p, hipStream_t s) {
   const long long heads = (long long)p.B * p.H;
   const int batches = p.into == p.cache ? 1 : (p.keep + 1023) / 1024;
-  if (heads > INT_MAX || heads * batches * 2 > INT_MAX) return -1;
+  if (!grid_ok(heads * batches * 2, kEvictThreads)) return kCacheGrid;
   (void)hipGetLastError();
   // four waves meet sooner than sixteen, as long as they hold the candidates
   if (p.tiles * kCacheTile <= 256 * kEvictKeys)
@@ -1477,9 +1480,9 @@ template <int D>
 int launch_append(const CacheRows& p, hipStream_t s) {
   constexpr int ROWS = RowLanes<D>::ROWS, ITER = 64 / ROWS;
   const long long heads = (long long)p.B * p.H;
-  const bool many = p.n >= 64;
+  const bool many = p.n >= 64;   // (n: at most 2^30)
   const long long g = many ? heads * ((p.n + 63) / 64) : (heads * p.n + ROWS - 1) / ROWS;
-  if (g > INT_MAX) return -1;
+  if (!grid_ok(g, 256)) return kCacheGrid;
   (void)hipGetLastError();
   const dim3 grid((unsigned)g), block(256);
   if (many && heads * p.n * 4 * D > kStreamBytes)
@@ -1495,9 +1498,11 @@ template <int D>
 int launch_read(const CacheRows& p, hipStream_t s) {
   const long long rows = (long long)p.B * p.H * p.n;
   const long long g = (rows + RowLanes<D>::ROWS - 1) / RowLanes<D>::ROWS;
-  if (g > INT_MAX) return -1;
+  // (137 GB of values are more workgroups than one dimension holds)
+  const long long gx = std::min(g, 1LL << 23), gy = (g + gx - 1) / gx;
+  if (gy > 65535) return kCacheGrid;
   (void)hipGetLastError();
-  const dim3 grid((unsigned)g), block(256);
+  const dim3 grid((unsigned)gx, (unsigned)gy), block(256);
   // (4 x 32 heads x 4,096 rows of 128, 268 MB of values: 58 -> 49 us)
   if (rows * 4 * D > kStreamBytes) hipLaunchKernelGGL((cache_read_kernel<D, true>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((cache_read_kernel<D, false>), grid, block, 0, s, p);

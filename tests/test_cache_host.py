@@ -224,3 +224,25 @@ except (F.FabftError, TypeError) as e:
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, text=True, capture_output=True, timeout=600)
     assert r.returncode == 0 and r.stdout.startswith("refused:"), r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("call,kw", [
+    # rows whose 32-bit indexes would overflow
+    (append, dict(n=(1 << 30) + 1)), (append, dict(n=(1 << 31) - 1, strides=[0] * 6)),
+    (read, dict(n=(1 << 31) - 1)), (attn, dict(Lq=(1 << 31) - 1)), (attn, dict(G=(1 << 30) + 1)),
+    # more workgroups than a grid holds: 2^24 of 256 threads, 2^22 of 1,024
+    (append, dict(B=1 << 12, H=1 << 12, n=64)), (append, dict(B=1 << 12, H=1 << 11, d=256, n=63)),
+    (attn, dict(B=1 << 12, H=1 << 12)), (attn, dict(B=1 << 10, H=1 << 10, nsplit=16, capacity=1024)),
+    (attn, dict(B=1 << 12, H=1 << 12, G=64)), (attn, dict(B=1 << 12, H=1 << 12, weight=P)),
+    (evict, dict(B=1 << 10, H=1 << 11, weight=BIG, into=1 << 50, into_weight=1 << 60)),
+], ids=str)
+def test_more_than_a_launch_holds(call, kw):
+    assert call(**kw) == F.E_SHAPE
+
+
+def test_row_counts_of_the_sizes():
+    for f, last in ((F.cache_workspace_bytes, (64, 2)), (F.cache_splits, (64,))):
+        assert f(1, 1, 1, 1 << 30, *last) > 0 and f(1, 1, 1 << 15, 1 << 15, *last) > 0
+        for args in ((1, 1, 1, (1 << 31) - 1), (1, 1, 1 << 15, (1 << 15) + 1), (2, 1, 1, 1 << 30)):
+            with pytest.raises(F.FabftError):
+                f(*args, *last)

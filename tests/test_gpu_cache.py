@@ -109,6 +109,21 @@ def test_read_zeros_outside():
     assert np.array_equal(v[1, 0, :3], v0[1, 0, 60:63]) and np.all(v[1, 0, 3:] == 0)
 
 
+def test_read_of_more_than_a_grid_dimension():
+    """More rows than one dimension of a grid has workgroups for: 2^29 before the cache's 64."""
+    far = 1 << 29
+    if torch.cuda.mem_get_info()[0] < 180 << 30:
+        pytest.skip("needs 130 GiB of device memory")
+    c, k0, v0 = filled(1, 1, 64, 64, 8)
+    kr, vr = F.cache_read(c, ints([-far - 36]), far + 100)
+    for x, e in ((kr, k0), (vr, v0)):
+        assert np.array_equal(G.from_dev_bf16(x[:, :, far + 36:]), e)
+        y = x[0, 0, :far + 36].view(torch.int32).flatten()
+        assert not any(bool(p.any()) for p in y.split(1 << 30))
+    del kr, vr, x, y
+    torch.cuda.empty_cache()
+
+
 def test_append_strides():
     """[B, n, H, d] projections seen as [B, H, n, d], a slice of wider rows, one row for all heads."""
     B, H, n, d = 2, 3, 5, 96
