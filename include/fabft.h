@@ -453,7 +453,8 @@ int fabft_attn_fwd_debug(const void* q, const void* k, const void* v,
  * x / scale goes to the nearest number of the grid, ties to the even code. All
  * values are bf16 numbers. K's 32 channels, or V's row, with a NaN or an
  * infinity among them read as NaN, and the query rows that see such a key are
- * flagged FABFT_FLAG_NONFINITE.
+ * flagged FABFT_FLAG_NONFINITE (for V: unless the key's softmax weight
+ * underflows to 0 in fp32).
  *
  * With each row of V the cache keeps the sum of its codes, taken when the row
  * is appended, which is what the checksum's prediction is made of: besides
@@ -505,7 +506,8 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * behind them are padding and get O = 0, resid = 0, flag 0, as do rows that see
  * no key. causal != 0: the query rows are the last counts[b] keys of the
  * sequence, row i sees slots <= lengths[b] - counts[b] + i. O, resid, flags, the
- * threshold and the weighted check as in fabft_attn_fwd; the score check and
+ * threshold and the weighted check as in fabft_attn_fwd, but that a row of keys whose
+ * scores are all -infinity (an overflow) is NaN and flagged FABFT_FLAG_NONFINITE; the score check and
  * the algorithm setting do not apply. Weights (times V's scale) are rounded to
  * bf16 for the P V product; o and c use the same ones, l the unrounded.
  *

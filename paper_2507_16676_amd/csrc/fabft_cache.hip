@@ -360,7 +360,11 @@ struct RowEnd {
   __device__ static __forceinline__ void run(const CacheParams& p, size_t row, int lane, int last,
                                              const float (&o)[CPL], float m, float l, float c,
                                              float cw) {
-    const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;   // (l NaN: NaN)
+    float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;   // (l NaN: NaN)
+    // keys, but l = 0: every score overflowed to -inf, and no weight is a number
+    uint32_t none = last >= 0 && (__float_as_uint(l) << 1) == 0 ? 0x7fc00000u : 0u;
+    asm volatile("" : "+v"(none));   // (as in nonfinite_bits)
+    inv = __uint_as_float(__float_as_uint(inv) | none);
     float act = 0.f, absum = 0.f, actw = 0.f, x[CPL];
 #pragma unroll
     for (int j = 0; j < CPL; ++j) {

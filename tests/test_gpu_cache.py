@@ -319,6 +319,32 @@ def test_nan_keys_leave_the_weights(rows):
     assert abs(float(w[0, 1].double().sum()) - 0.5 * cap - G * int((~seen).sum())) < 1e-3
 
 
+@pytest.mark.parametrize("nsplit", [1, 16])
+@pytest.mark.parametrize("G_,Lq", [(1, 1), (2, 2), (8, 5)])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_scores_that_overflow(d, G_, Lq, nsplit):
+    """Rows whose scores are all -inf have no weights: NaN and flagged, and they add nothing to
+    the keys' weights; with some at -inf those keys have the weight 0."""
+    cap, n = 4096, 4000
+    x = torch.full((1, 2, n, d), 1e38, dtype=torch.bfloat16, device="cuda")
+    x[0, 1, ::2] = 2.0 ** -100      # head 1: every other key has a finite score, about 0
+    v = draw(33, 1, 2, n, d)
+    c = F.cache_new(1, 2, cap, d)
+    F.cache_append(c, x, v, ints([0]))
+    q = torch.full((1, 2 * G_, Lq, d), -1e38, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(1, 2, cap, device="cuda")
+    o, _, flags = F.attn_fwd_cache(q, c, ints([n]), scale=2.0 ** -40, weight=w, nsplit=nsplit)
+    assert bool(torch.isnan(o[:, :G_]).all()) and bool((flags[:, :G_] == 3).all())
+    assert bool((w[0, 0] == 0).all())
+    assert int(flags[:, G_:].sum()) == 0
+    mean = oracle.cache_v(G.from_dev_bf16(v))[0, 1, ::2].mean(axis=0)
+    # the weights are equal: fp32 sums of 2,000 of them, and the rounding of O
+    err = np.abs(G.from_dev_bf16(o[:, G_:]) - mean)
+    assert np.all(err <= 2.0 ** -8 * np.abs(mean) + 2.0 ** -12 * np.abs(v.float().cpu().numpy()).max())
+    assert bool((w[0, 1, 1::2] == 0).all())
+    assert torch.allclose(w[0, 1, :n:2], torch.tensor(G_ * Lq / 2000.0, device="cuda"), rtol=2.0 ** -10)
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_attention_peaked(d):
     """Scores that jump late past the lazily kept maximum, and far below it."""
