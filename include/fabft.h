@@ -517,8 +517,8 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * decay (finite, >= 0; else FABFT_E_SCALE) 0 overwrites. Slots from lengths[b] on
  * stay as they were. Each slot's sum has one fixed order.
  *
- * nsplit: 1..64 ranges of whole 64-key tiles per row, merged by the last
- * workgroup of a row to finish; fabft_cache_splits gives the library's choice. A workspace
+ * nsplit: 1..64 ranges of whole 64-key tiles per row, whose results are merged at
+ * the end; fabft_cache_splits gives the library's choice. A workspace
  * (16-byte aligned, overwritten) of fabft_cache_workspace_bytes bytes is needed
  * where that is not 0 (nsplit > 1, or with weight). B * H * G * Lq is at most 2^30
  * (FABFT_E_SHAPE). q and o must not overlap.

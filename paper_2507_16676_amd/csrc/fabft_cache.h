@@ -92,17 +92,24 @@ struct CacheEvict {
 inline int cache_row_tile(int R) { return R <= 1 ? 1 : R <= 4 ? 4 : R <= 8 ? 8 : R <= 16 ? 16 : 32; }
 // As many tiles stay with one workgroup: a merge costs 2.2 us, a round of tiles 0.9.
 constexpr int kCacheFewTiles = 12;
-// Splits of the keys of a cache of `tiles` tiles: two workgroups per CU (512) while each has 16
-// tiles or more, four for each of its waves, else one per CU. Measured (us, splits at 512 and
-// at 256 workgroups): 128 heads of 512 tiles 109 113, 64 of 512 30.0 33.4, 128 of 128 30.8
-// 32.0; 32 heads of 65 tiles 13.1 11.8, 64 of 32 13.1 12.7, 8 heads of 512 21.6 18.4.
+// Splits of the keys of a cache of `tiles` tiles, a tile for each wave or more: so many that the
+// workgroups fill the chip once, and no round of a few is left over. Up to 16 rows: two
+// workgroups per CU (512) while each has 16 tiles or more, else one. Measured (us, splits
+// at 512 and at 256 workgroups): 128 heads of 512 tiles 109 113, 64 of 512 30.0 33.4, 128 of 128
+// 30.8 32.0; 32 heads of 65 tiles 13.1 11.8, 64 of 32 13.1 12.7, 8 heads of 512 21.6 18.4. Rounded
+// down and up: 96 heads of 512 tiles 75.0 91.2, 132 of 256 56.8 80.3, 192 of 128 46.2 52.9, 288
+// of 64 36.7 44.3.
+// More rows: no more than one per CU, since the records are more too. (256 row tiles of 128
+// channels: 64 tiles of keys 34.9 in one split, 51.8 in two, 256 tiles 104 and 114, 512 tiles 177
+// and 177; 192 row tiles of 64 channels, 64 tiles, 27.9, 40.9 and 46.2 in three; 64 row tiles,
+// 128 tiles, 28.7 in four splits, 29.7 in eight.)
 inline int cache_splits(int B, int H, int R, int tiles) {
   if (tiles <= kCacheFewTiles) return 1;
   const long long units = (long long)B * H * ((R + cache_row_tile(R) - 1) / cache_row_tile(R));
-  long long ns = (512 + units - 1) / units;
-  if (tiles < 16 * ns) ns = (256 + units - 1) / units;
+  long long ns = (R > 16 ? 256 : 512) / units;
+  if (R <= 16 && tiles < 16 * ns) ns = 256 / units;
   if (ns > (tiles + 3) / 4) ns = (tiles + 3) / 4;
-  return ns > 64 ? 64 : (int)ns;
+  return ns > 64 ? 64 : ns < 1 ? 1 : (int)ns;
 }
 inline int cache_record_floats(int d) { return d + 4; }
 

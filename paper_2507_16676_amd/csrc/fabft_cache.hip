@@ -643,48 +643,44 @@ __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& s
                                              int rows_most, int ns, float* ex, float* st_w) {
   constexpr int RS = D + 4, C4 = D / 4, CPL = RowEnd<D>::CPL, W = kAttnWaves, K = 16 / W;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int rows = min(rows_most, p.R - r0);
-  for (int b0 = 0; b0 < rows; b0 += 16) {   // 16 rows at a time
-    const int nr = min(16, rows - b0);
-    const float* rec = p.ws + (row0 + r0 + b0) * p.nsplit * RS;
-    f32x4 h[K];
+  const int nr = min(rows_most, p.R - r0);   // at most 16
+  const float* rec = p.ws + (row0 + r0) * p.nsplit * RS;
+  f32x4 h[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int i = wave + W * k;
-      h[k] = f32x4{-kInf, 0.f, 0.f, 0.f};
-      if (i < nr && lane < ns)
-        h[k] = *reinterpret_cast<const f32x4*>(rec + ((size_t)i * p.nsplit + lane) * RS);
-    }
-    float m[K], l[K], c[K], cw[K];
+  for (int k = 0; k < K; ++k) {
+    const int i = wave + W * k;
+    h[k] = f32x4{-kInf, 0.f, 0.f, 0.f};
+    if (i < nr && lane < ns)
+      h[k] = *reinterpret_cast<const f32x4*>(rec + ((size_t)i * p.nsplit + lane) * RS);
+  }
+  float m[K], l[K], c[K], cw[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      m[k] = wave_max(h[k][0]);
-      const float w = h[k][0] == -kInf ? (nonfinite_bits(h[k][1]) ? 1.f : 0.f)
-                                       : __builtin_amdgcn_exp2f(h[k][0] - m[k]);
-      l[k] = wave_sum(w * h[k][1]);
-      c[k] = wave_sum(w * h[k][2]);
-      cw[k] = wave_sum(w * h[k][3]);
-      st_w[(wave + W * k) * 64 + lane] = w;
-    }
-    __syncthreads();
-    for (int e = tid; e < nr * C4; e += 64 * W) {
-      const int i = e / C4;
-      const float* a = rec + (size_t)i * p.nsplit * RS + 4 + 4 * (e - i * C4);
-      *reinterpret_cast<f32x4*>(ex + i * RS + 4 * (e - i * C4)) =
-          ns <= 8 ? merge_columns<8>(a, RS, ns, st_w + i * 64) : merge_columns<32>(a, RS, ns, st_w + i * 64);
-    }
-    __syncthreads();
+  for (int k = 0; k < K; ++k) {
+    m[k] = wave_max(h[k][0]);
+    const float w = h[k][0] == -kInf ? (nonfinite_bits(h[k][1]) ? 1.f : 0.f)
+                                     : __builtin_amdgcn_exp2f(h[k][0] - m[k]);
+    l[k] = wave_sum(w * h[k][1]);
+    c[k] = wave_sum(w * h[k][2]);
+    cw[k] = wave_sum(w * h[k][3]);
+    st_w[(wave + W * k) * 64 + lane] = w;
+  }
+  __syncthreads();
+  for (int e = tid; e < nr * C4; e += 64 * W) {
+    const int i = e / C4;
+    const float* a = rec + (size_t)i * p.nsplit * RS + 4 + 4 * (e - i * C4);
+    *reinterpret_cast<f32x4*>(ex + i * RS + 4 * (e - i * C4)) =
+        ns <= 8 ? merge_columns<8>(a, RS, ns, st_w + i * 64) : merge_columns<32>(a, RS, ns, st_w + i * 64);
+  }
+  __syncthreads();
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int i = wave + W * k;
-      if (i < nr) {
-        float y[CPL];
+  for (int k = 0; k < K; ++k) {
+    const int i = wave + W * k;
+    if (i < nr) {
+      float y[CPL];
 #pragma unroll
-        for (int j = 0; j < CPL; ++j) y[j] = lane < RowEnd<D>::LANES ? ex[i * RS + CPL * lane + j] : 0.f;
-        RowEnd<D>::run(p, row0 + r0 + b0 + i, lane, seen.last(p, r0 + b0 + i), y, m[k], l[k], c[k], cw[k]);
-      }
+      for (int j = 0; j < CPL; ++j) y[j] = lane < RowEnd<D>::LANES ? ex[i * RS + CPL * lane + j] : 0.f;
+      RowEnd<D>::run(p, row0 + r0 + i, lane, seen.last(p, r0 + i), y, m[k], l[k], c[k], cw[k]);
     }
-    __syncthreads();
   }
 }
 
@@ -957,7 +953,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
       }
     }
   }
-  if (ns == 1 || !p.tickets) return;
+  if (RP == 32 || ns == 1 || !p.tickets) return;
   // the last of the row tile's workgroups to come here merges the splits
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of the records is out
   __syncthreads();
@@ -1163,9 +1159,10 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   const dim3 grid((unsigned)g), block(64 * kAttnWaves);
   // One CU takes 60 GB/s or so from beyond its L2: with 530 KB of records a row tile (16 rows of
   // 256, 32 splits) the call took 32 us with the merge in the last workgroup and 23 with it as a
-  // launch of its own, with 135 KB (32 rows of 128, 8 splits) 66 and 60, with 67 KB (4 rows, 32
-  // splits) 16.9 and 17.2.
-  const bool apart = p0.nsplit > 1 && (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000;
+  // launch of its own, with 67 KB (4 rows, 32 splits) 16.9 and 17.2. Of more than
+  // 16 rows always: 32 of 128, 4 splits (64 row tiles), 35.1 and 28.7.
+  const bool apart =
+      p0.nsplit > 1 && (rt == 32 || (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000);
   if (!grid_ok(g, 64 * kAttnWaves) || (apart && !grid_ok(mg, 256)) || (p0.weight && !grid_ok(heads * ch, 256)))
     return kCacheGrid;
   CacheParams p = p0;
