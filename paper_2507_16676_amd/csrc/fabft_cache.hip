@@ -638,12 +638,13 @@ __device__ __forceinline__ f32x4 merge_columns(const float* a, size_t step, int 
 // {l, o, c, c_w} (c merges like one more column of o, Eq. 10), then the rows' ends. One
 // workgroup reads all records from beyond its L2, so what counts is how many loads it has in
 // flight: a thread takes four columns of a row over up to 32 splits at once.
+constexpr int kMergeRows = 8;   // of the row tiles that merge so
 template <int D>
 __device__ __forceinline__ void merge_splits(const CacheParams& p, const Seen& seen, size_t row0, int r0,
                                              int rows_most, int ns, float* ex, float* st_w) {
-  constexpr int RS = D + 4, C4 = D / 4, CPL = RowEnd<D>::CPL, W = kAttnWaves, K = 16 / W;
+  constexpr int RS = D + 4, C4 = D / 4, CPL = RowEnd<D>::CPL, W = kAttnWaves, K = kMergeRows / W;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nr = min(rows_most, p.R - r0);   // at most 16
+  const int nr = min(rows_most, p.R - r0);
   const float* rec = p.ws + (row0 + r0) * p.nsplit * RS;
   f32x4 h[K];
 #pragma unroll
@@ -703,9 +704,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
   constexpr int XLDS = R::COLS * RS * 4;
   __shared__ __align__(16) uint8_t lds[kAttnWaves * (VLDS + PLDS > XLDS ? VLDS + PLDS : XLDS)];
   __shared__ f32x4 st[kAttnWaves][16];
-  __shared__ float st_w[16 * 64];
+  __shared__ float st_w[kMergeRows * 64];
   __shared__ int last_one;
-  static_assert(sizeof(lds) >= 16 * RS * 4 || R::COLS < 16, "merge_splits");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int id = blockIdx.x;
@@ -953,7 +953,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
       }
     }
   }
-  if (RP == 32 || ns == 1 || !p.tickets) return;
+  if (RP > kMergeRows || ns == 1 || !p.tickets) return;
   // the last of the row tile's workgroups to come here merges the splits
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of the records is out
   __syncthreads();
@@ -1157,12 +1157,13 @@ int launch_attn(const CacheParams& p0, hipStream_t s) {
   if (ch > most) ch = most;
   (void)hipGetLastError();
   const dim3 grid((unsigned)g), block(64 * kAttnWaves);
-  // One CU takes 60 GB/s or so from beyond its L2: with 530 KB of records a row tile (16 rows of
-  // 256, 32 splits) the call took 32 us with the merge in the last workgroup and 23 with it as a
-  // launch of its own, with 67 KB (4 rows, 32 splits) 16.9 and 17.2. Of more than
-  // 16 rows always: 32 of 128, 4 splits (64 row tiles), 35.1 and 28.7.
+  // One CU takes 60 GB/s or so from beyond its L2: with 135 KB of records a row tile (32 rows of
+  // 128, 8 splits) the call took 66 us with the merge in the last workgroup and 60 with it as a
+  // launch of its own, with 67 KB (4 rows, 32 splits) 16.9 and 17.2. Of 16 rows and more always:
+  // 16 of 64, 16 splits, 16.1 and 14.2, 128 row tiles of 16, 4 splits, 27.2 and 25.4 (192 in two
+  // splits 53 and 55), 64 row tiles of 32, 4 splits, 35.1 and 28.7.
   const bool apart =
-      p0.nsplit > 1 && (rt == 32 || (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000);
+      p0.nsplit > 1 && (rt > kMergeRows || (long long)std::min(rt, p0.R) * p0.nsplit * (D + 4) * 4 > 100000);
   if (!grid_ok(g, 64 * kAttnWaves) || (apart && !grid_ok(mg, 256)) || (p0.weight && !grid_ok(heads * ch, 256)))
     return kCacheGrid;
   CacheParams p = p0;
