@@ -649,3 +649,39 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of different shapes, splits and merges with one workspace, replayed in turn
+    and between eager calls with it: each result is the one of a call by itself."""
+    calls, graphs = [], []
+    shapes = [(2, 2, 1, 1, 4096, 128, 8), (1, 3, 4, 2, 2048, 64, 16), (2, 1, 4, 8, 2048, 128, 5),
+              (3, 2, 2, 1, 1024, 256, 4)]
+    need = max(F.cache_workspace_bytes(B, H, Gq, Lq, d, ns, True) for B, H, Gq, Lq, _, d, ns in shapes)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for i, (B, H, Gq, Lq, cap, d, ns) in enumerate(shapes):
+        c = filled(B, H, cap, d, 60 + 3 * i)[0]
+        q, lens = draw(80 + i, B, H * Gq, Lq, d), ints([cap - 5 * b for b in range(B)])
+        w = torch.zeros((B, H, cap), device="cuda")
+        kw = dict(causal=True, nsplit=ns, decay=0.0)
+        w1 = torch.full_like(w, 7)      # (slots behind the lengths stay as they are below)
+        alone = (*F.attn_fwd_cache(q, c, lens, weight=w1, **kw), w1)
+        out = tuple(torch.empty_like(x) for x in alone[:3])
+        call = lambda q=q, c=c, lens=lens, w=w, out=out, kw=kw: F.attn_fwd_cache(
+            q, c, lens, weight=w, workspace=ws, out=out, **kw)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call()
+        graphs.append(g)
+        calls.append((call, (*out, w), alone))
+    n = len(calls)
+    for turn in range(12):
+        for j in range(n):
+            i = (j * (1 + turn % 3) + turn) % n
+            call, got, alone = calls[i]
+            for x in got:
+                x.fill_(7)
+            graphs[i].replay() if (turn + j) % 3 else call()
+            assert all(torch.equal(x, y) for x, y in zip(got, alone)), (turn, i)
