@@ -468,11 +468,12 @@ int fabft_attn_fwd_debug(const void* q, const void* k, const void* v,
  * slots (keys) per head. The library keeps no lengths: every call is told them
  * in device arrays of B ints, so that it can be captured into a graph whose
  * replays see their current values. A slot that was never written may hold
- * anything. All four calls are asynchronous on the library stream. More than a
- * launch holds (2^32 threads; FABFT_E_SHAPE, and nothing ran) is 2^24 workgroups:
- * of append 64 rows of a head (n < 64: 2048 / d rows), of the attention a split of
- * 1, 4, 8, 16 or 32 query rows; 2^21 heads, or more and 1024 slots of a head each,
- * of evict.
+ * anything. All four calls are asynchronous on the library stream. A call
+ * that needs 2^32 threads is refused (FABFT_E_SHAPE) and does nothing. That is
+ * 2^24 workgroups of append (each 64 rows of a head; where n < 64, 32 rows at
+ * d = 64, 8 at 256, else 16) or of the attention (1, 4, 8, 16 or 32 query rows of
+ * a key/value head, one split), and 2^21 heads of evict (into another cache:
+ * 2^21 times 1024 slots).
  */
 long long fabft_cache_bytes(int B, int H, int capacity, int d);
 
