@@ -917,13 +917,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, D == 256 && RP == 32 ? 1 : 2) void
       const int r = r0 + 16 * n + i;
       if (r >= p.R) break;   // wave-uniform, as all below
       const int lr = seen.last(p, r);
-      float mm = -kInf;
-#pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) mm = __builtin_fmaxf(mm, st[w][i][0]);
-      float x[CPL], ls = 0.f, cs = 0.f, cw = 0.f;
+      // a row that sees no key: m = -inf and zeros, whatever its q made of the keys that the
+      // tile's other rows see (m = +inf would be NaN where splits are merged)
+      float mm = -kInf, x[CPL], ls = 0.f, cs = 0.f, cw = 0.f;
 #pragma unroll
       for (int j = 0; j < CPL; ++j) x[j] = 0.f;
       if (lr >= 0) {
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) mm = __builtin_fmaxf(mm, st[w][i][0]);
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) {
           const f32x4 sw = st[w][i];

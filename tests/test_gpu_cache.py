@@ -421,6 +421,54 @@ def test_masked_places_hold_anything():
         assert bool((w2[0, :, :200].sum(-1) - 0.25 * 200 - 6).abs().max() < 1e-3)
 
 
+# Row tiles with rows that see no key, where splits are merged: rows of a workgroup (1 has no
+# such row beside others), a merge in the last workgroup and by a launch of its own
+PADDED = [
+    # B, H, G, Lq, capacity, d, causal, lengths, counts, nsplit
+    (4, 2, 1, 1, 1088, 128, True, [1088, 1000, 833, 900], [1, 0, 1, 0], 4),
+    (3, 2, 1, 4, 1088, 128, True, [1088, 1000, 833], [2, 0, 9], 4),
+    (2, 1, 3, 2, 1600, 96, False, [1599, 900], [1, 2], 6),
+    (2, 2, 2, 4, 1152, 256, False, [1150, 1000], [3, 1], 5),
+    (2, 2, 4, 3, 2048, 64, True, [2000, 850], [1, 2], 8),            # 12 rows: apart
+    (2, 1, 2, 8, 1344, 256, False, [1344, 1100], [5, 8], 4),         # 16 rows: apart
+    (3, 1, 1, 20, 1280, 64, True, [1280, 900, 1000], [7, 19, 0], 5),
+    (2, 2, 3, 30, 1408, 128, False, [1400, 1000], [29, 3], 4),       # several row tiles
+    (1, 1, 2, 801, 832, 64, True, [800], [801], 4),                  # row 0 sees no key beside row 800
+]
+
+
+@pytest.mark.parametrize("case", PADDED, ids=lambda c: "b{}h{}g{}q{}c{}d{}".format(*c[:6]))
+def test_rows_without_keys_beside_others(case):
+    """Rows behind the counts, and causal rows before the first key, are O = 0, resid = 0, flag 0
+    whatever their q holds, and change nothing else: bit for bit as with zeros there."""
+    B, H, Gq, Lq, cap, d, causal, lengths, counts, ns = case
+    print(f"[cache rows without keys] {case}", flush=True)
+    assert ns > 1 and min(lengths) > 12 * F.CACHE_TILE      # (fewer tiles are not split)
+    c, ke, ve = filled(B, H, cap, d, 47)
+    q = draw(48, B, H * Gq, Lq, d)
+    cnt = [min(n, Lq) for n in counts]
+    none = torch.zeros((B, Lq), dtype=torch.bool)
+    for b in range(B):
+        for i in range(Lq):
+            none[b, i] = i >= cnt[b] or (causal and lengths[b] - cnt[b] + i < 0)
+    none = none[:, None].expand(B, H * Gq, Lq).cuda()
+    assert bool(none.any()) and not bool(none.all())
+    q[none] = 0
+    w0 = torch.rand((B, H, cap), device="cuda")
+    weight = w0.clone()
+    a = check_attention(q, c, ke, ve, lengths, cnt, causal, d ** -0.5, weight=weight, nsplit=ns)
+    assert not bool(a[0][none].any()) and not bool(a[1][none].any())
+    inf = float("inf")
+    for x in (inf, -inf, 3e38, -3e38, float("nan")):
+        for every in (1, 7):              # the whole row, or some channels (NaN from inf * 0 too)
+            p, w = q.clone(), w0.clone()
+            p[none] = torch.where(torch.arange(d, device="cuda") % every == 0, x, 0.5).to(p.dtype)
+            o, resid, flags = F.attn_fwd_cache(p, c, ints(lengths), counts=ints(counts), causal=causal,
+                                               scale=d ** -0.5, nsplit=ns, weight=w)
+            assert not bool(flags.any()), (x, every, flags.nonzero()[:3])
+            assert torch.equal(o, a[0]) and torch.equal(resid, a[1]) and torch.equal(w, weight)
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_changed_codes_are_flagged(d):
     """A bit of V's codes, or of their sums, that changed in memory since the append fails the
