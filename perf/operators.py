@@ -111,6 +111,13 @@ def _sizes(case):
     return tuple(case[k] for k in ("B", "H", "G", "d", "L", "Lq"))
 
 
+def _slots(case):
+    """Slots per head of the cache before the call. All Lq rows of a padded step are appended and
+    read back, those behind a sequence's own ones too: they have room."""
+    room = case["Lq"] if case["kind"] == "step" and case["pad"] else 0
+    return -(-(case["L"] + room) // 64) * 64
+
+
 def _host_lengths(case, seed):
     """Keys per sequence, and query rows (or new tokens) per sequence."""
     B, L, Lq = case["B"], case["L"], case["Lq"]
@@ -140,13 +147,13 @@ def _inputs(case, seed):
     k, v = normal(B, H, L, d), normal(B, H, L, d)
     k *= torch.exp(0.5 * normal(1, H, 1, d))
     k *= 1 + 3 * (torch.rand((B, H, L, 1), generator=g, device="cuda") < 0.01)
-    w = torch.exp(torch.randn((B, H, -(-L // 64) * 64), generator=g, device="cuda"))
+    w = torch.exp(torch.randn((B, H, _slots(case)), generator=g, device="cuda"))
     return q, k, v, w
 
 
 def prepare(case, seed):
     B, H, G, d, L, Lq = _sizes(case)
-    kind, C = case["kind"], -(-L // 64) * 64
+    kind, C = case["kind"], _slots(case)
     q, k, v, w = _inputs(case, seed)
     lengths, counts = _host_lengths(case, seed)
     dev = {"device": "cuda", "dtype": torch.int32}
