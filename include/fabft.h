@@ -522,7 +522,7 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * the end; fabft_cache_splits gives the library's choice. A workspace
  * (16-byte aligned, overwritten) of fabft_cache_workspace_bytes bytes is needed
  * where that is not 0 (nsplit > 1, or with weight). B * H * G * Lq is at most 2^30
- * (FABFT_E_SHAPE). q and o must not overlap.
+ * (FABFT_E_SHAPE). q and o must not overlap (FABFT_E_SHAPE).
  */
 int fabft_attn_fwd_cache(const void* q, const void* cache, void* o,
                          float* resid, uint8_t* flags, int B, int H, int G,

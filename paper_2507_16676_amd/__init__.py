@@ -693,7 +693,7 @@ def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
     of each key summed over the rows of its group (decay 0 overwrites; rows with a flag add nothing;
     slots from lengths[b] on stay as they were). nsplit: ranges of the keys, by default
     cache_splits(...). workspace: optional GPU tensor of cache_workspace_bytes(...) bytes. out:
-    optional preallocated (o, resid, flags)."""
+    optional preallocated (o, resid, flags); o must not overlap q."""
     c, dev = cache, _device_of(cache)
     if not isinstance(q, _torch.Tensor) or q.dtype is not _torch.bfloat16:
         raise TypeError("q must be a torch.bfloat16 tensor")
@@ -725,6 +725,8 @@ def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
         o = _check_out(out[0], "out[0] (o)", q.shape, _torch.bfloat16, dev)
         resid = _check_out(out[1], "out[1] (resid)", (B, HG, Lq), f32, dev)
         flags = _check_out(out[2], "out[2] (flags)", (B, HG, Lq), _torch.uint8, dev)
+        if abs(o.data_ptr() - q.data_ptr()) < 2 * q.numel():
+            raise ValueError("out[0] (o) must not overlap q")
     else:
         o, resid, flags = _outputs(q, B, HG, Lq)
     _call(dev, "fabft_attn_fwd_cache", _LIB.fabft_attn_fwd_cache, q.data_ptr(), c.data.data_ptr(),

@@ -513,7 +513,7 @@ const char* fabft_status_str(int status) {
   switch (status) {
     case FABFT_OK: return "ok";
     case FABFT_E_NULL: return "null pointer argument";
-    case FABFT_E_SHAPE: return "invalid shape (B, H, Lq, Lk must be >= 1; grid too large)";
+    case FABFT_E_SHAPE: return "invalid shape (B, H, Lq, Lk must be >= 1; grid too large) or buffers that overlap";
     case FABFT_E_HEADDIM: return "unsupported head dimension (d must be 64, 96, 128 or 256)";
     case FABFT_E_ALIGN: return "q, k, v and o must be 16-byte aligned";
     case FABFT_E_LAUNCH: return "kernel launch failed";
@@ -661,6 +661,9 @@ int fabft_attn_fwd_cache(const void* q, const void* cache, void* o, float* resid
   if (need > 0 && !workspace) return FABFT_E_NULL;
   if (!aligned16(q) || !aligned16(o) || (need > 0 && !aligned16(workspace))) return FABFT_E_ALIGN;
   if (workspace_bytes < need) return FABFT_E_WORKSPACE;
+  // (the weights' pass reads q when o is written)
+  const long long qbytes = 2LL * B * H * G * Lq * d;
+  if (overlap(q, qbytes, o, qbytes)) return FABFT_E_SHAPE;
   fabft::CacheParams p{};
   p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
   p.q = static_cast<const uint16_t*>(q);

@@ -246,3 +246,30 @@ def test_row_counts_of_the_sizes():
         for args in ((1, 1, 1, (1 << 31) - 1), (1, 1, 1 << 15, (1 << 15) + 1), (2, 1, 1, 1 << 30)):
             with pytest.raises(F.FabftError):
                 f(*args, *last)
+
+
+@pytest.mark.parametrize("weight", [None, BIG])
+@pytest.mark.parametrize("q,o", [(P, P), (P, P + 16), (P + 2 * 3 * 4 * 5 * 128 - 16, P)])
+def test_outputs_over_the_queries_are_refused(q, o, weight):
+    """The second pass of a call with weights reads q again."""
+    assert attn(q=q, o=o, B=2, H=3, G=4, Lq=5, weight=weight) == F.E_SHAPE
+
+
+def test_outputs_over_the_queries_are_refused_by_the_binding():
+    code = f"CALLS = {['f(q, 0)', 'f(q, 0, weight=w)', 'f(q, 64)', 'f(q, -64)']!r}\n" + PROLOGUE.split("bad = object()")[0] + """
+buf = t(3 * 2 * 3 * 4 * 64)
+n = 2 * 3 * 4 * 64
+q = buf[n:2 * n].view(2, 3, 4, 64)
+def f(q, by, **kw):
+    out = (buf[n + by:2 * n + by].view(2, 3, 4, 64), t(2, 3, 4, dtype=torch.float32),
+           t(2, 3, 4, dtype=torch.uint8))
+    return F.attn_fwd_cache(q, c, i(), out=out, **kw)
+for call in CALLS:
+    try:
+        eval(call)
+        print("passed")
+    except ValueError as e:
+        print("overlap" in str(e))
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, text=True, capture_output=True, timeout=600)
+    assert r.returncode == 0 and r.stdout.split() == ["True"] * 4, r.stdout + r.stderr

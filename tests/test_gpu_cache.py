@@ -514,6 +514,26 @@ def test_workspace_and_out():
     assert torch.equal(o, o2)
 
 
+def test_output_beside_the_queries():
+    """q and o next to each other in one buffer, either way round; over each other they are refused."""
+    B, H, cap, d, Lq = 2, 2, 1024, 64, 3
+    c, ke, ve = filled(B, H, cap, d, 45)
+    n = B * 2 * H * Lq * d
+    x = draw(46, B, 2 * H, Lq, d)
+    for at, to in ((0, n), (n, 0)):
+        buf = torch.zeros(2 * n, dtype=torch.bfloat16, device="cuda")
+        q, o = (buf[i:i + n].view(B, 2 * H, Lq, d) for i in (at, to))
+        q.copy_(x)
+        out = (o, torch.empty((B, 2 * H, Lq), device="cuda"),
+               torch.empty((B, 2 * H, Lq), dtype=torch.uint8, device="cuda"))
+        check_attention(q, c, ke, ve, [1000, 900], None, True, 0.125, nsplit=4, out=out,
+                        weight=torch.zeros((B, H, cap), device="cuda"))
+        assert torch.equal(q, x)
+        for bad in (q, buf[n // 2:n // 2 + n].view_as(q)):
+            with pytest.raises(ValueError):
+                F.attn_fwd_cache(q, c, ints([1000, 900]), out=(bad, *out[1:]))
+
+
 def test_offsets_past_32_bits():
     """One head of 34 million slots (4.8 GB): rows at its far end are written, read and attended."""
     cap, d, n = 34_000_000 // 64 * 64, 128, 100
