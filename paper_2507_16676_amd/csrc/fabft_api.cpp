@@ -520,7 +520,7 @@ const char* fabft_status_str(int status) {
     case FABFT_E_SCALE: return "scale (and decay) must be finite and >= 0";
     case FABFT_E_FAULT: return "fault descriptor out of range";
     case FABFT_E_THRESHOLD: return "threshold must be >= 0";
-    case FABFT_E_WORKSPACE: return "workspace too small (see fabft_splitkv_workspace_bytes)";
+    case FABFT_E_WORKSPACE: return "workspace too small (see fabft_splitkv_workspace_bytes, fabft_cache_workspace_bytes)";
     case FABFT_E_MODE: return "mode argument out of range";
     default: return "unknown status";
   }

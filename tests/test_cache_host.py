@@ -273,3 +273,8 @@ for call in CALLS:
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, text=True, capture_output=True, timeout=600)
     assert r.returncode == 0 and r.stdout.split() == ["True"] * 4, r.stdout + r.stderr
+
+
+def test_workspace_error_names_its_sizes():
+    with pytest.raises(F.FabftError, match="fabft_cache_workspace_bytes"):
+        F._check(attn(nsplit=2, workspace_bytes=0), "fabft_attn_fwd_cache")
