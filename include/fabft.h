@@ -511,6 +511,11 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * scores are all -infinity (an overflow) is NaN and flagged FABFT_FLAG_NONFINITE; the score check and
  * the algorithm setting do not apply. Weights (times V's scale) are rounded to
  * bf16 for the P V product; o and c use the same ones, l the unrounded.
+ * The fp32 sums of o and c are divided by l at the end, and a weight is up to 2^8 until
+ * then: they are finite as long as the keys of a row times the largest sum of |v_j| over
+ * a row of V stay below 2^118. Larger ones can overflow, also where O is a finite number;
+ * the row is then flagged FABFT_FLAG_NONFINITE. Times the smallest scale, 2^-100, weights below
+ * 2^-26 of the row's largest may count as 0.
  *
  * weight (may be NULL): fp32 [B, H, capacity]; for every slot k < lengths[b]
  *   weight_k <- decay * weight_k + sum of P_ik over the rows of the G heads

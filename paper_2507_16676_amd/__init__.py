@@ -687,7 +687,8 @@ def attn_fwd_cache(q, cache: Cache, lengths, counts=None, causal: bool = False,
     """Flash-ABFT forward over the 4-bit cache. q: bfloat16 [B, H * G, Lq, d], contiguous, G query
     heads per key/value head. lengths: int32 [B] on the GPU, the keys of each sequence; counts:
     int32 [B], its query rows (the others are padding: O = 0, no flag). causal: the query rows are
-    the last counts[b] keys. Returns (o, resid, flags) as attn_fwd.
+    the last counts[b] keys. Returns (o, resid, flags) as attn_fwd; where a row's number of keys times
+    the largest sum of |v| over a row of V passes 2^118, its sums can overflow (FLAG_NONFINITE).
 
     weight: optional fp32 [B, H, capacity], updated in place: decay * weight + the softmax weights
     of each key summed over the rows of its group (decay 0 overwrites; rows with a flag add nothing;

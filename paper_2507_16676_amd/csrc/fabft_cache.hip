@@ -34,7 +34,11 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 constexpr float kInf = __builtin_inff();
-constexpr float kLazy = 8.0f;   // max drift (exp2 domain) before a rescale, as in the forward
+// Max drift (exp2 domain) before a rescale, as in the forward: e is up to 2^8, p' = bf16(e s) up to
+// 2^8 s, and o and c, sums over n keys, are below 2^10 n S with S the largest sum of |v| over a row (c
+// holds hi, up to 16 above the sum of the codes): finite for n S < 2^118. A smaller e (2^-38 of it
+// for every length) would take as much from the other end, where s is 2^-100 and p' 2^-126 at e = 2^-26.
+constexpr float kLazy = 8.0f;
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),

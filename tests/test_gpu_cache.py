@@ -1,6 +1,8 @@
 """The 4-bit key/value cache on the GPU through the package: append and read
 value by value, the attention against the fp64 oracle on the cache's values,
 the keys' weights, eviction, and a decode loop that uses all of them."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -365,6 +367,43 @@ def test_attention_value_sizes():
         c = F.cache_new(B, H, cap, d)
         F.cache_append(c, k, v, ints([0]))
         check_attention(draw(19, B, H, 3, d), c, *values(k, v), [250], None, True, d ** -0.5)
+
+
+@pytest.mark.parametrize("nsplit", [1, 2])
+@pytest.mark.parametrize("G_,Lq", [(1, 1), (2, 2), (1, 8), (2, 8), (4, 8)])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_values_up_to_the_bound(d, G_, Lq, nsplit):
+    """Keys times the largest sum of |v| over a row just below 2^118, with scores that rise by
+    almost 8 (base 2) behind every wave's first tile, where the kept maximum does not follow: right.
+    Far above: rows whose sums overflow are flagged, and the others right."""
+    H, cap = 2, 1024
+    n = 1000
+    k = torch.zeros((1, H, n, d), dtype=torch.bfloat16, device="cuda")
+    k[:, :, 64 * 4 * nsplit:] = 1.0
+    q = torch.ones((1, H * G_, Lq, d), dtype=torch.bfloat16, device="cuda")
+    scale = 7.9 * math.log(2) / d
+    v0 = draw(20, 1, H, n, d).abs().clamp(0.25, 4.0)
+    total = float(oracle.cache_v(G.from_dev_bf16(v0)).sum(-1).max()) * n
+    top = 117 - math.floor(math.log2(total))
+    assert 2.0 ** 117 <= total * 2.0 ** top < 2.0 ** 118
+    for e in (top, -90):
+        c = F.cache_new(1, H, cap, d)
+        v = v0 * 2.0 ** e
+        F.cache_append(c, k, v, ints([0]))
+        whole = (np.pad(x, ((0, 0), (0, 0), (0, cap - n), (0, 0))) for x in values(k, v))
+        check_attention(q, c, *whole, [n], None, False, scale, nsplit=nsplit,
+                        weight=torch.zeros((1, H, cap), device="cuda"))
+    for e in range(top + 1, 125, 3):
+        c = F.cache_new(1, H, cap, d)
+        v = v0 * 2.0 ** e
+        F.cache_append(c, k, v, ints([0]))
+        o, _, flags = F.attn_fwd_cache(q, c, ints([n]), scale=scale, nsplit=nsplit)
+        bad = (flags & F.FLAG_NONFINITE) != 0
+        assert bool(torch.isfinite(o)[~bad].all())
+        eo, ea, _, _ = oracle.cache_attention(np.ones((G_, Lq, d)), *(x[0, 0] for x in values(k, v)), n, Lq,
+                                              False, scale)
+        err = np.abs(G.from_dev_bf16(o[:, :G_])[0] - eo)[~bad[0, :G_].cpu().numpy()]
+        assert np.all(err <= 2.0 ** -6 * ea.max())
 
 
 def test_same_as_the_bf16_forward_on_the_read_values():
