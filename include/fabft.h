@@ -514,7 +514,9 @@ int fabft_cache_read(const void* cache, int B, int H, int capacity, int d,
  * The fp32 sums of o and c are divided by l at the end, and a weight is up to 2^8 until
  * then: they are finite as long as the keys of a row times the largest sum of |v_j| over
  * a row of V stay below 2^118. Larger ones can overflow, also where O is a finite number;
- * the row is then flagged FABFT_FLAG_NONFINITE. Times the smallest scale, 2^-100, weights below
+ * the row is then flagged FABFT_FLAG_NONFINITE. (This is for scores, times log2 e, below
+ * 2^20 in size. The exponents are rounded as numbers of that size: from 2^31 on a row can be
+ * NaN and flagged though its scores are finite.) Times the smallest scale, 2^-100, weights below
  * 2^-26 of the row's largest may count as 0.
  *
  * weight (may be NULL): fp32 [B, H, capacity]; for every slot k < lengths[b]

@@ -347,6 +347,35 @@ def test_scores_that_overflow(d, G_, Lq, nsplit):
     assert torch.allclose(w[0, 1, :n:2], torch.tensor(G_ * Lq / 2000.0, device="cuda"), rtol=2.0 ** -10)
 
 
+@pytest.mark.parametrize("nsplit", [1, 4])
+@pytest.mark.parametrize("G_,Lq", [(1, 1), (2, 2), (2, 9)])
+def test_huge_scores(G_, Lq, nsplit):
+    """Scores of 2^20 to 2^60 whose largest is 2^-3 of them or more above the others: O is the V row of
+    that key, and from 2^31 on that or NaN and flagged."""
+    H, cap, n, d = 2, 1024, 1000, 64
+    at = 777
+    k = (torch.rand((1, H, n, 1), device="cuda") - 0.5).to(torch.bfloat16).expand(1, H, n, d).contiguous()
+    k[:, :, at] = 0.75                      # (the others: 0.5 at most)
+    v = draw(34, 1, H, n, d)
+    q = torch.ones((1, H * G_, Lq, d), dtype=torch.bfloat16, device="cuda")
+    c = F.cache_new(1, H, cap, d)
+    F.cache_append(c, k, v, ints([0]))
+    ve = oracle.cache_v(G.from_dev_bf16(v))[0, :, at]
+    for e in (20, 27, 30, 31, 33, 45, 60):
+        for sign in (1.0, 1.0 + 2.0 ** -20, 1.5):
+            scale = sign * 2.0 ** e * math.log(2) / (0.75 * d)
+            o, _, flags = F.attn_fwd_cache(q, c, ints([n]), scale=scale, nsplit=nsplit)
+            O = G.from_dev_bf16(o).reshape(H, -1, d)
+            f = flags.cpu().numpy().reshape(H, -1)
+            assert np.all((f == 0) | (f & F.FLAG_NONFINITE != 0))
+            if e <= 30:
+                assert np.all(f == 0)
+            for h in range(H):
+                ok = f[h] == 0
+                # one weight, rounded to bf16, and the rounding of O
+                assert np.all(np.abs(O[h][ok] - ve[h]) <= 2.0 ** -6 * np.abs(ve[h]))
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
 def test_attention_peaked(d):
     """Scores that jump late past the lazily kept maximum, and far below it."""
