@@ -102,7 +102,14 @@ constexpr int kCacheFewTiles = 12;
 // More rows: no more than one per CU, since the records are more too. (256 row tiles of 128
 // channels: 64 tiles of keys 34.9 in one split, 51.8 in two, 256 tiles 104 and 114, 512 tiles 177
 // and 177; 192 row tiles of 64 channels, 64 tiles, 27.9, 40.9 and 46.2 in three; 64 row tiles,
-// 128 tiles, 28.7 in four splits, 29.7 in eight.)
+// 128 tiles, 28.7 in four splits, 29.7 in eight.) Between 129 and 255 row tiles that is one split,
+// which leaves CUs without work; two, of 258 to 510 workgroups, are slower all the same up to 256
+// tiles of keys (d = 128, one and two splits: 130 row tiles 30.8 42.2 at 64 tiles, 48.9 58.6 at 128,
+// 85.5 91.2 at 256; 200 row tiles 31.1 47.3, 49.9 63.8, 85.9 96.3; d = 64, 256 tiles: 71.3 72.8 and
+// 70.9 78.2) and at 512 tiles between 8% faster and 10% slower (130 row tiles: d = 64 130 120, 128
+// 159 156; 200: 129 125, 159 161; 160: d = 96 146 141, 256 260 286). What rounding down costs: 128
+// row tiles of 512 tiles of keys take 75.3 (d = 64) and 97.5 (128) in the two splits chosen, 70.6 and
+// 92.5 in four; of 128 tiles 34.8 and 34.9, 40.3 and 40.5.
 inline int cache_splits(int B, int H, int R, int tiles) {
   if (tiles <= kCacheFewTiles) return 1;
   const long long units = (long long)B * H * ((R + cache_row_tile(R) - 1) / cache_row_tile(R));
